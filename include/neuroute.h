@@ -308,6 +308,161 @@ nr_status nr_lsim_grad_at(const float *d2_emb, const float *lat, int64_t B, int3
                           float gamma_rho, const double *tau_sq, double *num_cnt,
                           float *grad_lat, hipStream_t stream);
 
+/* ---- Layers of an encoder in training, and of encoders an index does not
+ * hold (their latents go to nr_search_ex as logits, their gradient starts from
+ * nr_lsim_grad).  Tensors are DEVICE memory, [rows x width] with a row stride
+ * `ld` (elements, >= width; the elements of a row are next to each other), of
+ * one type: NR_F32, NR_BF16 or NR_F16.  Pointers are aligned to their element;
+ * rows that start on 16-byte boundaries are read fastest.  Sums are held in
+ * fp32 and rounded to the type once; every result is the same bit for bit on
+ * every call with the same inputs.  Outputs must not overlap inputs or one
+ * another.  Widths are 1..NR_MAX_WIDTH, rows >= 0 (0 rows: no output rows, and
+ * gradients of parameters are zero).  `ws` is DEVICE scratch of at least the
+ * bytes that the call's _ws function names for the same description (16-byte
+ * aligned; NULL where that is 0), in use until the call's work is done: calls
+ * that may overlap in time, and captured graphs that may, need one each.
+ * Rows of a batch do not influence one another's outputs. */
+#define NR_MAX_WIDTH 16384
+enum { NR_BF16 = 2, NR_F16 = 3 };   /* further nr_dtype values, for the layers only */
+typedef enum {
+  NR_ACT_NONE = 0,
+  NR_ACT_RELU = 1,
+  NR_ACT_GELU = 2,               /* z Phi(z), Phi the normal distribution function */
+  NR_ACT_SILU = 3                /* z / (1 + exp(-z)) */
+} nr_act;
+
+/* Activations held in 8 bits between a forward pass and its backward pass: the
+ * elements of a row in groups of 32 (the last may be short), each held as
+ * q 2^e with one e per group:
+ *   NR_HOLD_I8    q an int8; e the smallest with max|x| 2^-e < 127.5
+ *   NR_HOLD_E4M3  q an fp8 of 4 exponent and 3 mantissa bits (OCP); e the
+ *                 smallest with max|x| 2^-e <= 448
+ * q is rounded to nearest, ties to even.  e lies in [-126, 121] (i8) or
+ * [-126, 119] (e4m3), for NR_F16 at most 9 or 7, so that every held value is
+ * finite in the type; magnitudes past the largest held one become that one.
+ * q 2^e is exact in fp32 and bf16.  A group with an infinity or a NaN is
+ * NaN as a whole.  Memory: q [rows x ldq] bytes with ldq = 32 ceil(width / 32)
+ * (zeros behind the width), 16-byte aligned; scale [rows x ldq / 32] bytes: e +
+ * 127, or 255 for NaN. */
+typedef enum { NR_HOLD_NONE = 0, NR_HOLD_I8 = 1, NR_HOLD_E4M3 = 2 } nr_hold;
+
+/* x [m x d] into 8 bits, and back (the type of y sets how it is rounded). */
+nr_status nr_act_hold(const void *x, int64_t ldx, int64_t m, int32_t d, int32_t dtype,
+                      int32_t hold, void *q, uint8_t *scale, hipStream_t stream);
+nr_status nr_act_read(const void *q, const uint8_t *scale, int64_t m, int32_t d, int32_t hold,
+                      int32_t dtype, void *y, int64_t ldy, hipStream_t stream);
+
+/* y = act(z) + residual, z = x w^T + bias (x [m x k], w [n x k], bias [n]; y, z
+ * and residual [m x n]).  bias, residual and pre may be NULL.  pre receives z
+ * for the backward pass, in the type (ldp) or held in 8 bits (pre_hold,
+ * pre_scale: as nr_act_hold holds z once it is rounded to the type). */
+typedef struct {
+  int64_t m;
+  int32_t n, k;
+  int32_t dtype;                  /* NR_F32, NR_BF16 or NR_F16 */
+  int32_t act;                    /* nr_act */
+  const void *x;
+  int64_t ldx;
+  const void *w;
+  int64_t ldw;
+  const void *bias;
+  const void *residual;
+  int64_t ldr;
+  void *y;
+  int64_t ldy;
+  void *pre;
+  int64_t ldp;
+  int32_t pre_hold;               /* nr_hold */
+  uint8_t *pre_scale;
+} nr_linear_desc;
+size_t nr_linear_ws(const nr_linear_desc *desc);
+nr_status nr_linear(const nr_linear_desc *desc, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* The gradients, dz = dy act'(z): dx = dz w, dw = dz^T x, db = sum of dz over
+ * the rows (the residual's gradient is dy).  Outputs that are NULL are left
+ * out.  pre is z (ignored for NR_ACT_NONE; for NR_ACT_RELU without a residual
+ * y serves as well, having the same sign); x is needed for dw, w for dx.  x and
+ * pre may be held in 8 bits.  In the 16-bit types dz is rounded to the type
+ * before the products, as their operands are. */
+typedef struct {
+  int64_t m;
+  int32_t n, k;
+  int32_t dtype;
+  int32_t act;
+  const void *dy;
+  int64_t lddy;
+  const void *x;
+  int64_t ldx;
+  int32_t x_hold;
+  const uint8_t *x_scale;
+  const void *w;
+  int64_t ldw;
+  const void *pre;
+  int64_t ldp;
+  int32_t pre_hold;
+  const uint8_t *pre_scale;
+  void *dx;                       /* [m x k] */
+  int64_t lddx;
+  void *dw;                       /* [n x k] */
+  int64_t lddw;
+  void *db;                       /* [n] */
+} nr_linear_grad_desc;
+size_t nr_linear_grad_ws(const nr_linear_grad_desc *desc);
+nr_status nr_linear_grad(const nr_linear_grad_desc *desc, void *ws, size_t ws_bytes,
+                         hipStream_t stream);
+
+/* Layer norm of every row: mean and rstd = 1 / sqrt(mean (x - mean)^2 + eps)
+ * over its d elements, y = (x - mean) rstd weight + bias (weight and bias [d],
+ * NULL for 1 and 0).  stats (fp32 [2 x m], NULL: not wanted) receives the means,
+ * then the rstds.  x_hold and y_hold ask for x and y in 8 bits too (xq, x_scale;
+ * yq, y_scale). */
+typedef struct {
+  int64_t m;
+  int32_t d;
+  int32_t dtype;
+  float eps;                      /* >= 0 and finite */
+  const void *x;
+  int64_t ldx;
+  const void *weight;
+  const void *bias;
+  void *y;
+  int64_t ldy;
+  float *stats;
+  int32_t x_hold, y_hold;
+  void *xq;
+  uint8_t *x_scale;
+  void *yq;
+  uint8_t *y_scale;
+} nr_layer_norm_desc;
+nr_status nr_layer_norm(const nr_layer_norm_desc *desc, hipStream_t stream);
+
+/* With xh = (x - mean) rstd and u = dy weight: dx = rstd (u - mean(u) - xh
+ * mean(u xh)) + add (add: the gradient that reaches x on another path, or NULL),
+ * dweight = sum of dy xh over the rows, dbias = sum of dy.  Outputs that are
+ * NULL are left out.  x may be held in 8 bits; stats are the forward pass's. */
+typedef struct {
+  int64_t m;
+  int32_t d;
+  int32_t dtype;
+  const void *dy;
+  int64_t lddy;
+  const void *x;
+  int64_t ldx;
+  int32_t x_hold;
+  const uint8_t *x_scale;
+  const float *stats;
+  const void *weight;
+  const void *add;
+  int64_t ldadd;
+  void *dx;
+  int64_t lddx;
+  void *dweight;
+  void *dbias;
+} nr_layer_norm_grad_desc;
+size_t nr_layer_norm_grad_ws(const nr_layer_norm_grad_desc *desc);
+nr_status nr_layer_norm_grad(const nr_layer_norm_grad_desc *desc, void *ws, size_t ws_bytes,
+                             hipStream_t stream);
+
 /* ---- Index construction on the GPU (Sec. 3.3 "Bucket allocation" and
  * "In-bucket clustering"; thresholds, Sec. 3.2.3).  Untimed, run once.
  * The latents of the base rows come from nr_encode on an encoder-only index

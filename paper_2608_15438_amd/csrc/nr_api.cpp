@@ -15,6 +15,7 @@
 #include <vector>
 
 #include "nr_internal.h"
+#include "nr_layers.h"
 
 namespace {
 
@@ -807,6 +808,113 @@ nr_status make_events(nr_index *ix, EventSet *es) {
 
 }  // namespace
 
+// ---- layers in training: argument checks
+
+namespace {
+
+bool layer_dtype(int32_t t) { return t == NR_F32 || t == NR_BF16 || t == NR_F16; }
+
+nr_status check_shape(int64_t m, int32_t w, const char *what) {
+  if (m < 0) return fail(NR_EINVAL, "rows %lld < 0", (long long)m);
+  if (w < 1) return fail(NR_EINVAL, "%s %d < 1", what, w);
+  if (w > NR_MAX_WIDTH) return fail(NR_EUNSUPPORTED, "%s %d > %d", what, w, NR_MAX_WIDTH);
+  if (m > ((int64_t)1 << 40)) return fail(NR_EUNSUPPORTED, "rows %lld > 2^40", (long long)m);
+  return NR_OK;
+}
+
+// a matrix of the type: there, aligned to its elements, its rows not overlapping
+nr_status check_mat(const void *p, int64_t ld, int64_t m, int32_t w, int32_t dtype,
+                    const char *what) {
+  if (m > 0 && !p) return fail(NR_EINVAL, "%s is NULL", what);
+  if (reinterpret_cast<uintptr_t>(p) % nr::layer_elem(dtype))
+    return fail(NR_EINVAL, "%s is not aligned to its elements", what);
+  if (ld < w && m > 1)
+    return fail(NR_EINVAL, "%s: row stride %lld < width %d", what, (long long)ld, w);
+  if (ld < 0 || ld > ((int64_t)1 << 40))
+    return fail(NR_EINVAL, "%s: row stride %lld out of range", what, (long long)ld);
+  return NR_OK;
+}
+
+nr_status check_held(const void *q, const uint8_t *scale, int64_t ld, int64_t m, int32_t w,
+                     int32_t hold, const char *what) {
+  if (hold != NR_HOLD_I8 && hold != NR_HOLD_E4M3)
+    return fail(NR_EINVAL, "%s: unknown 8-bit format %d", what, hold);
+  if (m > 0 && (!q || !scale)) return fail(NR_EINVAL, "%s or its scales are NULL", what);
+  if (reinterpret_cast<uintptr_t>(q) % 16) return fail(NR_EINVAL, "%s is not 16-byte aligned", what);
+  if (ld != nr::hold_ld(w))
+    return fail(NR_EINVAL, "%s: row stride %lld must be %lld", what, (long long)ld,
+                (long long)nr::hold_ld(w));
+  return NR_OK;
+}
+
+nr_status check_vec(const void *p, int32_t dtype, const char *what) {
+  if (reinterpret_cast<uintptr_t>(p) % nr::layer_elem(dtype))
+    return fail(NR_EINVAL, "%s is not aligned to its elements", what);
+  return NR_OK;
+}
+
+nr_status check_ws(const void *ws, size_t have, size_t need) {
+  if (need == 0) return NR_OK;
+  if (!ws || have < need)
+    return fail(NR_EINVAL, "work space of %zu bytes, %zu needed", ws ? have : (size_t)0, need);
+  if (reinterpret_cast<uintptr_t>(ws) % 16) return fail(NR_EINVAL, "work space is not 16-byte aligned");
+  return NR_OK;
+}
+
+#define NR_TRY(call)                 \
+  do {                               \
+    const nr_status st_ = (call);    \
+    if (st_ != NR_OK) return st_;    \
+  } while (0)
+
+nr_status check_linear(const nr_linear_desc *d) {
+  if (!d) return fail(NR_EINVAL, "NULL description");
+  if (!layer_dtype(d->dtype)) return fail(NR_EINVAL, "unknown type %d", d->dtype);
+  if (d->act < NR_ACT_NONE || d->act > NR_ACT_SILU) return fail(NR_EINVAL, "unknown act %d", d->act);
+  NR_TRY(check_shape(d->m, d->n, "n"));
+  return check_shape(d->m, d->k, "k");
+}
+
+nr_status check_linear_grad(const nr_linear_grad_desc *d) {
+  if (!d) return fail(NR_EINVAL, "NULL description");
+  if (!layer_dtype(d->dtype)) return fail(NR_EINVAL, "unknown type %d", d->dtype);
+  if (d->act < NR_ACT_NONE || d->act > NR_ACT_SILU) return fail(NR_EINVAL, "unknown act %d", d->act);
+  NR_TRY(check_shape(d->m, d->n, "n"));
+  return check_shape(d->m, d->k, "k");
+}
+
+nr::LinearGradArgs grad_args(const nr_linear_grad_desc *d) {
+  nr::LinearGradArgs a{};
+  a.m = d->m, a.n = d->n, a.k = d->k, a.act = d->act;
+  a.dy = d->dy, a.lddy = d->lddy;
+  a.x = nr::LayerMat{d->x, d->ldx, d->x_hold, d->x_scale};
+  a.w = d->w, a.ldw = d->ldw;
+  a.pre = nr::LayerMat{d->pre, d->ldp, d->pre_hold, d->pre_scale};
+  a.dx = d->dx, a.lddx = d->lddx;
+  a.dw = d->dw, a.lddw = d->lddw;
+  a.db = d->db;
+  return a;
+}
+
+nr_status check_norm(int64_t m, int32_t w, int32_t dtype) {
+  if (!layer_dtype(dtype)) return fail(NR_EINVAL, "unknown type %d", dtype);
+  return check_shape(m, w, "d");
+}
+
+nr::NormGradArgs norm_grad_args(const nr_layer_norm_grad_desc *d) {
+  nr::NormGradArgs a{};
+  a.m = d->m, a.d = d->d;
+  a.dy = d->dy, a.lddy = d->lddy;
+  a.x = nr::LayerMat{d->x, d->ldx, d->x_hold, d->x_scale};
+  a.mean = d->stats, a.rstd = d->stats ? d->stats + d->m : nullptr;
+  a.g = d->weight, a.add = d->add, a.ldadd = d->ldadd;
+  a.dx = d->dx, a.lddx = d->lddx;
+  a.dg = d->dweight, a.db = d->dbias;
+  return a;
+}
+
+}  // namespace
+
 extern "C" {
 
 const char *nr_status_string(nr_status s) {
@@ -1315,6 +1423,140 @@ nr_status nr_lsim_grad_at(const float *d2_emb, const float *lat, int64_t B, int3
   if (!d2_emb || !lat || !tau_sq || !num_cnt || !grad_lat) return fail(NR_EINVAL, "NULL buffer");
   HIP_OK(nr::launch_lsim_grad(d2_emb, lat, B, L, gamma_rho, 0.0f, tau_sq, num_cnt, grad_lat,
                               stream));
+  return NR_OK;
+}
+
+// ---- layers in training
+
+nr_status nr_act_hold(const void *x, int64_t ldx, int64_t m, int32_t d, int32_t dtype,
+                      int32_t hold, void *q, uint8_t *scale, hipStream_t stream) {
+  if (!layer_dtype(dtype)) return fail(NR_EINVAL, "unknown type %d", dtype);
+  NR_TRY(check_shape(m, d, "d"));
+  NR_TRY(check_mat(x, ldx, m, d, dtype, "x"));
+  NR_TRY(check_held(q, scale, nr::hold_ld(d), m, d, hold, "q"));
+  HIP_OK(nr::launch_hold(x, ldx, m, d, dtype, hold, (uint8_t *)q, scale, stream));
+  return NR_OK;
+}
+
+nr_status nr_act_read(const void *q, const uint8_t *scale, int64_t m, int32_t d, int32_t hold,
+                      int32_t dtype, void *y, int64_t ldy, hipStream_t stream) {
+  if (!layer_dtype(dtype)) return fail(NR_EINVAL, "unknown type %d", dtype);
+  NR_TRY(check_shape(m, d, "d"));
+  NR_TRY(check_held(q, scale, nr::hold_ld(d), m, d, hold, "q"));
+  NR_TRY(check_mat(y, ldy, m, d, dtype, "y"));
+  HIP_OK(nr::launch_read((const uint8_t *)q, scale, m, d, hold, dtype, y, ldy, stream));
+  return NR_OK;
+}
+
+size_t nr_linear_ws(const nr_linear_desc *d) {
+  return check_linear(d) == NR_OK ? nr::linear_ws(d->m, d->n, d->k, d->dtype) : 0;
+}
+
+nr_status nr_linear(const nr_linear_desc *d, void *ws, size_t ws_bytes, hipStream_t stream) {
+  NR_TRY(check_linear(d));
+  NR_TRY(check_mat(d->x, d->ldx, d->m, d->k, d->dtype, "x"));
+  NR_TRY(check_mat(d->w, d->ldw, d->n, d->k, d->dtype, "w"));
+  NR_TRY(check_vec(d->bias, d->dtype, "bias"));
+  if (d->residual) NR_TRY(check_mat(d->residual, d->ldr, d->m, d->n, d->dtype, "residual"));
+  NR_TRY(check_mat(d->y, d->ldy, d->m, d->n, d->dtype, "y"));
+  if (d->pre_hold)
+    NR_TRY(check_held(d->pre, d->pre_scale, d->ldp, d->m, d->n, d->pre_hold, "pre"));
+  else if (d->pre)
+    NR_TRY(check_mat(d->pre, d->ldp, d->m, d->n, d->dtype, "pre"));
+  NR_TRY(check_ws(ws, ws_bytes, nr::linear_ws(d->m, d->n, d->k, d->dtype)));
+  if (d->m == 0) return NR_OK;
+  nr::LinearArgs a{};
+  a.m = d->m, a.n = d->n, a.k = d->k, a.act = d->act;
+  a.x = d->x, a.ldx = d->ldx;
+  a.w = d->w, a.ldw = d->ldw;
+  a.bias = d->bias, a.res = d->residual, a.ldr = d->ldr;
+  a.y = d->y, a.ldy = d->ldy;
+  a.pre = d->pre, a.ldp = d->ldp, a.pre_hold = d->pre_hold, a.pre_scale = d->pre_scale;
+  HIP_OK(nr::launch_linear(a, d->dtype, ws, stream));
+  return NR_OK;
+}
+
+size_t nr_linear_grad_ws(const nr_linear_grad_desc *d) {
+  return check_linear_grad(d) == NR_OK ? nr::linear_grad_ws(grad_args(d), d->dtype) : 0;
+}
+
+nr_status nr_linear_grad(const nr_linear_grad_desc *d, void *ws, size_t ws_bytes,
+                         hipStream_t stream) {
+  NR_TRY(check_linear_grad(d));
+  if (!d->dx && !d->dw && !d->db) return NR_OK;
+  NR_TRY(check_mat(d->dy, d->lddy, d->m, d->n, d->dtype, "dy"));
+  if (d->act != NR_ACT_NONE) {
+    if (d->pre_hold)
+      NR_TRY(check_held(d->pre, d->pre_scale, d->ldp, d->m, d->n, d->pre_hold, "pre"));
+    else
+      NR_TRY(check_mat(d->pre, d->ldp, d->m, d->n, d->dtype, "pre"));
+  }
+  if (d->dx) {
+    NR_TRY(check_mat(d->w, d->ldw, d->n, d->k, d->dtype, "w"));
+    NR_TRY(check_mat(d->dx, d->lddx, d->m, d->k, d->dtype, "dx"));
+  }
+  if (d->dw) {
+    if (d->x_hold)
+      NR_TRY(check_held(d->x, d->x_scale, d->ldx, d->m, d->k, d->x_hold, "x"));
+    else
+      NR_TRY(check_mat(d->x, d->ldx, d->m, d->k, d->dtype, "x"));
+    NR_TRY(check_mat(d->dw, d->lddw, d->n, d->k, d->dtype, "dw"));
+  }
+  NR_TRY(check_vec(d->db, d->dtype, "db"));
+  const nr::LinearGradArgs a = grad_args(d);
+  NR_TRY(check_ws(ws, ws_bytes, nr::linear_grad_ws(a, d->dtype)));
+  HIP_OK(nr::launch_linear_grad(a, d->dtype, ws, stream));
+  return NR_OK;
+}
+
+nr_status nr_layer_norm(const nr_layer_norm_desc *d, hipStream_t stream) {
+  if (!d) return fail(NR_EINVAL, "NULL description");
+  NR_TRY(check_norm(d->m, d->d, d->dtype));
+  if (!(d->eps >= 0.0f) || !std::isfinite(d->eps)) return fail(NR_EINVAL, "eps must be finite and >= 0");
+  NR_TRY(check_mat(d->x, d->ldx, d->m, d->d, d->dtype, "x"));
+  NR_TRY(check_vec(d->weight, d->dtype, "weight"));
+  NR_TRY(check_vec(d->bias, d->dtype, "bias"));
+  NR_TRY(check_mat(d->y, d->ldy, d->m, d->d, d->dtype, "y"));
+  if (reinterpret_cast<uintptr_t>(d->stats) % 4) return fail(NR_EINVAL, "stats is not aligned");
+  if (d->x_hold)
+    NR_TRY(check_held(d->xq, d->x_scale, nr::hold_ld(d->d), d->m, d->d, d->x_hold, "xq"));
+  if (d->y_hold)
+    NR_TRY(check_held(d->yq, d->y_scale, nr::hold_ld(d->d), d->m, d->d, d->y_hold, "yq"));
+  nr::NormArgs a{};
+  a.m = d->m, a.d = d->d, a.eps = d->eps;
+  a.x = d->x, a.ldx = d->ldx, a.g = d->weight, a.b = d->bias;
+  a.y = d->y, a.ldy = d->ldy;
+  a.mean = d->stats, a.rstd = d->stats ? d->stats + d->m : nullptr;
+  a.x_hold = d->x_hold, a.y_hold = d->y_hold;
+  a.xq = (uint8_t *)d->xq, a.xs = d->x_scale, a.yq = (uint8_t *)d->yq, a.ys = d->y_scale;
+  HIP_OK(nr::launch_norm(a, d->dtype, stream));
+  return NR_OK;
+}
+
+size_t nr_layer_norm_grad_ws(const nr_layer_norm_grad_desc *d) {
+  return d && check_norm(d->m, d->d, d->dtype) == NR_OK ? nr::norm_grad_ws(norm_grad_args(d)) : 0;
+}
+
+nr_status nr_layer_norm_grad(const nr_layer_norm_grad_desc *d, void *ws, size_t ws_bytes,
+                             hipStream_t stream) {
+  if (!d) return fail(NR_EINVAL, "NULL description");
+  NR_TRY(check_norm(d->m, d->d, d->dtype));
+  if (!d->dx && !d->dweight && !d->dbias) return NR_OK;
+  NR_TRY(check_mat(d->dy, d->lddy, d->m, d->d, d->dtype, "dy"));
+  if (d->x_hold)
+    NR_TRY(check_held(d->x, d->x_scale, d->ldx, d->m, d->d, d->x_hold, "x"));
+  else
+    NR_TRY(check_mat(d->x, d->ldx, d->m, d->d, d->dtype, "x"));
+  if (d->m > 0 && !d->stats) return fail(NR_EINVAL, "stats is NULL");
+  if (reinterpret_cast<uintptr_t>(d->stats) % 4) return fail(NR_EINVAL, "stats is not aligned");
+  NR_TRY(check_vec(d->weight, d->dtype, "weight"));
+  if (d->add) NR_TRY(check_mat(d->add, d->ldadd, d->m, d->d, d->dtype, "add"));
+  if (d->dx) NR_TRY(check_mat(d->dx, d->lddx, d->m, d->d, d->dtype, "dx"));
+  NR_TRY(check_vec(d->dweight, d->dtype, "dweight"));
+  NR_TRY(check_vec(d->dbias, d->dtype, "dbias"));
+  const nr::NormGradArgs a = norm_grad_args(d);
+  NR_TRY(check_ws(ws, ws_bytes, nr::norm_grad_ws(a)));
+  HIP_OK(nr::launch_norm_grad(a, d->dtype, ws, stream));
   return NR_OK;
 }
 

@@ -20,7 +20,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 SO_PATH = os.path.join(_HERE, "libneuroute.so")
 
 NR_OK, NR_EINVAL, NR_ENOMEM, NR_EDEVICE, NR_EUNSUPPORTED, NR_ECORRUPT = range(6)
-NR_U8, NR_F32 = 0, 1
+NR_U8, NR_F32, NR_BF16, NR_F16 = 0, 1, 2, 3
+NR_MAX_WIDTH = 16384
 NR_MAX_LAYERS = 8
 NR_MAX_KNOTS = 32
 NR_MAX_K = 64
@@ -40,6 +41,8 @@ WORK = ("tiles", "rows", "rows_read", "own_rows", "shared_rows", "shared_pairs",
 EXPORTS = ("nr_index_upload", "nr_index_free", "nr_search", "nr_search_ex", "nr_search_noalloc",
            "nr_encode", "nr_calibrate", "nr_pair_sqdist_ws", "nr_pair_sqdist", "nr_lsim_grad",
            "nr_pair_quantile_ws", "nr_pair_quantile", "nr_lsim_grad_at",
+           "nr_act_hold", "nr_act_read", "nr_linear_ws", "nr_linear", "nr_linear_grad_ws",
+           "nr_linear_grad", "nr_layer_norm", "nr_layer_norm_grad_ws", "nr_layer_norm_grad",
            "nr_build_tau", "nr_build_codes", "nr_build_plan", "nr_build_index",
            "nr_probe", "nr_route", "nr_route_capacity", "nr_refine", "nr_profile_enable",
            "nr_profile_read", "nr_last_work", "nr_stream_read", "nr_status_string",
@@ -92,6 +95,37 @@ class nr_params(C.Structure):
                 ("m_x", C.c_float * NR_MAX_KNOTS), ("m_y", C.c_float * NR_MAX_KNOTS)]
 
 
+_I, _N, _P = C.c_int64, C.c_int32, C.c_void_p
+
+
+class nr_linear_desc(C.Structure):
+    _fields_ = [("m", _I), ("n", _N), ("k", _N), ("dtype", _N), ("act", _N), ("x", _P),
+                ("ldx", _I), ("w", _P), ("ldw", _I), ("bias", _P), ("residual", _P), ("ldr", _I),
+                ("y", _P), ("ldy", _I), ("pre", _P), ("ldp", _I), ("pre_hold", _N),
+                ("pre_scale", _P)]
+
+
+class nr_linear_grad_desc(C.Structure):
+    _fields_ = [("m", _I), ("n", _N), ("k", _N), ("dtype", _N), ("act", _N), ("dy", _P),
+                ("lddy", _I), ("x", _P), ("ldx", _I), ("x_hold", _N), ("x_scale", _P), ("w", _P),
+                ("ldw", _I), ("pre", _P), ("ldp", _I), ("pre_hold", _N), ("pre_scale", _P),
+                ("dx", _P), ("lddx", _I), ("dw", _P), ("lddw", _I), ("db", _P)]
+
+
+class nr_layer_norm_desc(C.Structure):
+    _fields_ = [("m", _I), ("d", _N), ("dtype", _N), ("eps", C.c_float), ("x", _P), ("ldx", _I),
+                ("weight", _P), ("bias", _P), ("y", _P), ("ldy", _I), ("stats", _P),
+                ("x_hold", _N), ("y_hold", _N), ("xq", _P), ("x_scale", _P), ("yq", _P),
+                ("y_scale", _P)]
+
+
+class nr_layer_norm_grad_desc(C.Structure):
+    _fields_ = [("m", _I), ("d", _N), ("dtype", _N), ("dy", _P), ("lddy", _I), ("x", _P),
+                ("ldx", _I), ("x_hold", _N), ("x_scale", _P), ("stats", _P), ("weight", _P),
+                ("add", _P), ("ldadd", _I), ("dx", _P), ("lddx", _I), ("dweight", _P),
+                ("dbias", _P)]
+
+
 _lib = None
 
 
@@ -124,6 +158,17 @@ def lib():
         L.nr_pair_quantile_ws.restype = C.c_size_t
         L.nr_pair_quantile.argtypes = [P, C.c_int64, C.c_int64, C.c_float, P, P, P]
         L.nr_lsim_grad_at.argtypes = [P, P, C.c_int64, C.c_int32, C.c_float, P, P, P, P]
+        L.nr_act_hold.argtypes = [P, C.c_int64, C.c_int64, C.c_int32, C.c_int32, C.c_int32, P, P, P]
+        L.nr_act_read.argtypes = [P, P, C.c_int64, C.c_int32, C.c_int32, C.c_int32, P, C.c_int64, P]
+        L.nr_linear_ws.argtypes = [C.POINTER(nr_linear_desc)]
+        L.nr_linear.argtypes = [C.POINTER(nr_linear_desc), P, C.c_size_t, P]
+        L.nr_linear_grad_ws.argtypes = [C.POINTER(nr_linear_grad_desc)]
+        L.nr_linear_grad.argtypes = [C.POINTER(nr_linear_grad_desc), P, C.c_size_t, P]
+        L.nr_layer_norm.argtypes = [C.POINTER(nr_layer_norm_desc), P]
+        L.nr_layer_norm_grad_ws.argtypes = [C.POINTER(nr_layer_norm_grad_desc)]
+        L.nr_layer_norm_grad.argtypes = [C.POINTER(nr_layer_norm_grad_desc), P, C.c_size_t, P]
+        for name in ("nr_linear_ws", "nr_linear_grad_ws", "nr_layer_norm_grad_ws"):
+            getattr(L, name).restype = C.c_size_t
         L.nr_build_tau.argtypes = [P, C.c_int64, C.c_int32, P, P]
         L.nr_build_codes.argtypes = [P, C.c_int64, C.c_int32, P, P, P, P]
         L.nr_build_plan.argtypes = [P, C.c_int64, C.c_int32, C.c_int32, C.c_uint32, P, P,
@@ -296,6 +341,317 @@ def nr_build_index(desc: nr_build_desc, row_ids, bc_off, cl_off, centroids, stre
     _check(lib().nr_build_index(C.byref(desc), _ptr(row_ids), _ptr(bc_off), _ptr(cl_off),
                                 _ptr(centroids), C.byref(nc), _stream(stream)), "nr_build_index")
     return nc.value
+
+
+# --------------------------------------------------------------------------
+# layers in training
+# --------------------------------------------------------------------------
+
+LAYER_DTYPES = {torch.float32: NR_F32, torch.bfloat16: NR_BF16, torch.float16: NR_F16}
+ACTS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+HOLDS = {"i8": 1, "e4m3": 2}
+_HOLD_DTYPES = {"i8": torch.int8, "e4m3": torch.float8_e4m3fn}
+
+
+@dataclass
+class Held:
+    """An activation [m, d] in 8 bits (nr_act_hold): q [m, 32 ceil(d / 32)] int8 or
+    float8_e4m3fn and a scale byte per row and group of 32; `dtype` is the
+    type it came from.  The element is q * 2^(scale - 127), NaN where scale is 255."""
+    q: torch.Tensor
+    scale: torch.Tensor
+    d: int
+    fmt: str
+    dtype: torch.dtype
+
+    @property
+    def shape(self):
+        return (self.q.shape[0], self.d)
+
+    @property
+    def device(self):
+        return self.q.device
+
+    @classmethod
+    def empty(cls, m: int, d: int, fmt: str, dtype, device) -> "Held":
+        ldq = (d + 31) // 32 * 32
+        return cls(torch.empty((m, ldq), dtype=_HOLD_DTYPES[fmt], device=device),
+                   torch.empty((m, ldq // 32), dtype=torch.uint8, device=device), d, fmt, dtype)
+
+
+class _On:
+    """The device and stream of a call: outputs and work space are allocated on
+    that stream, so the allocator hands their memory on in its order."""
+
+    def __init__(self, t, stream):
+        self.dev = t.device
+        self.stream = stream
+        self.ctx = None
+
+    def __enter__(self):
+        if self.stream is not None:
+            if self.stream.device != self.dev:
+                raise ValueError(f"the stream is on {self.stream.device}, the tensors on {self.dev}")
+            self.ctx = torch.cuda.stream(self.stream)
+        elif self.dev.index != torch.cuda.current_device():
+            self.ctx = torch.cuda.device(self.dev)
+        if self.ctx is not None:
+            self.ctx.__enter__()
+        return C.c_void_p(torch.cuda.current_stream(self.dev).cuda_stream)
+
+    def __exit__(self, *e):
+        if self.ctx is not None:
+            self.ctx.__exit__(*e)
+
+
+def _mat(t, name, dtype, device, m=None, w=None):
+    """(pointer, row stride) of a device matrix whose rows' elements are next to
+    each other."""
+    if t.dim() != 2 or (m is not None and t.shape[0] != m) or (w is not None and t.shape[1] != w):
+        raise ValueError(f"{name} must be [{'m' if m is None else m}, {'d' if w is None else w}], "
+                         f"got {list(t.shape)}")
+    if not t.is_cuda or t.dtype != dtype or t.device != device:
+        raise ValueError(f"{name} must be {dtype} on {device}, got {t.dtype} on {t.device}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: the elements of a row must be next to each other")
+    ld = t.stride(0)
+    if t.shape[0] > 1 and ld < t.shape[1]:
+        raise ValueError(f"{name}: its rows overlap")
+    return t.data_ptr(), max(ld, t.shape[1]) if t.shape[0] <= 1 else ld
+
+
+def _vec(t, name, dtype, device, n):
+    if t is None:
+        return None
+    if tuple(t.shape) != (n,) or not t.is_cuda or t.dtype != dtype or t.device != device:
+        raise ValueError(f"{name} must be {dtype} [{n}] on {device}, "
+                         f"got {t.dtype} {list(t.shape)} on {t.device}")
+    if n > 1 and t.stride(0) != 1:
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _held(h, name, dtype, device, m, d):
+    """(q pointer, q's row stride, format, scale pointer)"""
+    ldq = (d + 31) // 32 * 32
+    if h.fmt not in HOLDS or h.shape != (m, d) or h.dtype != dtype or h.device != device:
+        raise ValueError(f"{name} must hold {dtype} [{m}, {d}] on {device}, got {h.fmt} of "
+                         f"{h.dtype} {list(h.shape)} on {h.device}")
+    _fits(h.q, f"{name}.q", _HOLD_DTYPES[h.fmt], m, ldq)
+    _fits(h.scale, f"{name}.scale", torch.uint8, m, ldq // 32)
+    if h.scale.device != device:
+        raise ValueError(f"{name}.scale must be on {device}")
+    return h.q.data_ptr(), ldq, HOLDS[h.fmt], h.scale.data_ptr()
+
+
+def _layer_input(t, name):
+    """The input that sets a call's shape, type and device."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype not in LAYER_DTYPES:
+        raise ValueError(f"{name}: {t.dtype} is none of float32, bfloat16 and float16")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be a matrix, got {list(t.shape)}")
+    return t.dtype, t.device
+
+
+def _act(act):
+    if act not in ACTS:
+        raise ValueError(f"act must be one of {sorted(ACTS)}, got {act!r}")
+    return ACTS[act]
+
+
+def _fmt(fmt, name):
+    if fmt not in HOLDS:
+        raise ValueError(f"{name} must be one of {sorted(HOLDS)}, got {fmt!r}")
+    return fmt
+
+
+def _work(nbytes, device):
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+
+
+def nr_act_hold(x: torch.Tensor, fmt: str = "i8", stream=None) -> Held:
+    """x [m, d] in 8 bits: groups of 32 along a row share a power of two."""
+    dtype, dev = _layer_input(x, "x")
+    _fmt(fmt, "fmt")
+    m, d = x.shape
+    p, ld = _mat(x, "x", dtype, dev)
+    with _On(x, stream) as s:
+        h = Held.empty(m, d, fmt, dtype, dev)
+        _check(lib().nr_act_hold(p, ld, m, d, LAYER_DTYPES[dtype], HOLDS[fmt], h.q.data_ptr(),
+                                 h.scale.data_ptr(), s), "nr_act_hold")
+    return h
+
+
+def nr_act_read(held: Held, dtype=None, stream=None) -> torch.Tensor:
+    """The values that `held` stands for, in its own type or another."""
+    dtype = held.dtype if dtype is None else dtype
+    if dtype not in LAYER_DTYPES:
+        raise ValueError(f"{dtype} is none of float32, bfloat16 and float16")
+    m, d = held.shape
+    q, ldq, fmt, scale = _held(held, "held", held.dtype, held.device, m, d)
+    with _On(held, stream) as s:
+        y = torch.empty((m, d), dtype=dtype, device=held.device)
+        _check(lib().nr_act_read(q, scale, m, d, fmt, LAYER_DTYPES[dtype], y.data_ptr(), d, s),
+               "nr_act_read")
+    return y
+
+
+def nr_linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None,
+              act: str = "none", residual: Optional[torch.Tensor] = None, pre=False, stream=None):
+    """act(x w^T + bias) + residual for x [m, k], w [n, k].  pre=True also returns
+    x w^T + bias for the backward pass, pre="i8" or "e4m3" the same in 8 bits."""
+    dtype, dev = _layer_input(x, "x")
+    m, k = x.shape
+    d = nr_linear_desc()
+    d.x, d.ldx = _mat(x, "x", dtype, dev)
+    if w.dim() != 2:
+        raise ValueError(f"w must be a matrix, got {list(w.shape)}")
+    n = w.shape[0]
+    d.w, d.ldw = _mat(w, "w", dtype, dev, n, k)
+    d.m, d.n, d.k, d.dtype, d.act = m, n, k, LAYER_DTYPES[dtype], _act(act)
+    d.bias = _vec(bias, "bias", dtype, dev, n)
+    if residual is not None:
+        d.residual, d.ldr = _mat(residual, "residual", dtype, dev, m, n)
+    if pre is not True and pre is not False:
+        _fmt(pre, "pre")
+    with _On(x, stream) as s:
+        y = torch.empty((m, n), dtype=dtype, device=dev)
+        d.y, d.ldy = y.data_ptr(), n
+        z = None
+        if pre is True:
+            z = torch.empty((m, n), dtype=dtype, device=dev)
+            d.pre, d.ldp = z.data_ptr(), n
+        elif pre:
+            z = Held.empty(m, n, pre, dtype, dev)
+            d.pre, d.ldp, d.pre_hold, d.pre_scale = (z.q.data_ptr(), z.q.shape[1], HOLDS[pre],
+                                                     z.scale.data_ptr())
+        L = lib()
+        nb = L.nr_linear_ws(C.byref(d))
+        ws = _work(nb, dev)
+        _check(L.nr_linear(C.byref(d), None if ws is None else ws.data_ptr(), nb, s), "nr_linear")
+    return y if z is None else (y, z)
+
+
+def nr_linear_grad(dy: torch.Tensor, x, w: Optional[torch.Tensor], act: str = "none", pre=None,
+                   dx: bool = True, dw: bool = True, db: bool = True, stream=None):
+    """(dx, dw, db) of nr_linear, None for those not asked for.  x and pre (z =
+    x w^T + bias; not needed for act="none") may be Held; x may be None without
+    dw, w without dx (but one of the two is needed for their width)."""
+    dtype, dev = _layer_input(dy, "dy")
+    m, n = dy.shape
+    d = nr_linear_grad_desc()
+    d.dy, d.lddy = _mat(dy, "dy", dtype, dev)
+    d.m, d.n, d.dtype, d.act = m, n, LAYER_DTYPES[dtype], _act(act)
+    if (x is None and (dw or w is None)) or (w is None and dx):
+        raise ValueError("dw needs x, dx needs w, and one of the two sets the width")
+    k = x.shape[1] if x is not None else w.shape[1]
+    d.k = k
+    if isinstance(x, Held):
+        d.x, d.ldx, d.x_hold, d.x_scale = _held(x, "x", dtype, dev, m, k)
+    elif x is not None:
+        d.x, d.ldx = _mat(x, "x", dtype, dev, m, k)
+    if w is not None:
+        d.w, d.ldw = _mat(w, "w", dtype, dev, n, k)
+    if act != "none":
+        if pre is None:
+            raise ValueError(f"act={act!r} needs pre")
+        if isinstance(pre, Held):
+            d.pre, d.ldp, d.pre_hold, d.pre_scale = _held(pre, "pre", dtype, dev, m, n)
+        else:
+            d.pre, d.ldp = _mat(pre, "pre", dtype, dev, m, n)
+    with _On(dy, stream) as s:
+        gx = torch.empty((m, k), dtype=dtype, device=dev) if dx else None
+        gw = torch.empty((n, k), dtype=dtype, device=dev) if dw else None
+        gb = torch.empty(n, dtype=dtype, device=dev) if db else None
+        if dx:
+            d.dx, d.lddx = gx.data_ptr(), k
+        if dw:
+            d.dw, d.lddw = gw.data_ptr(), k
+        if db:
+            d.db = gb.data_ptr()
+        L = lib()
+        nb = L.nr_linear_grad_ws(C.byref(d))
+        ws = _work(nb, dev)
+        _check(L.nr_linear_grad(C.byref(d), None if ws is None else ws.data_ptr(), nb, s),
+               "nr_linear_grad")
+    return gx, gw, gb
+
+
+def nr_layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None,
+                  bias: Optional[torch.Tensor] = None, eps: float = 1e-5, stats: bool = False,
+                  hold_x: Optional[str] = None, hold_y: Optional[str] = None, stream=None):
+    """Layer norm of the rows of x [m, d].  Returns y, and with it, in this order,
+    what else is asked for: stats (fp32 [2, m]: means and 1 / standard deviations,
+    for the backward pass), x and y in 8 bits (hold_x, hold_y: "i8" or "e4m3")."""
+    dtype, dev = _layer_input(x, "x")
+    m, w = x.shape
+    d = nr_layer_norm_desc()
+    d.m, d.d, d.dtype, d.eps = m, w, LAYER_DTYPES[dtype], eps
+    d.x, d.ldx = _mat(x, "x", dtype, dev)
+    d.weight = _vec(weight, "weight", dtype, dev, w)
+    d.bias = _vec(bias, "bias", dtype, dev, w)
+    for f, name in ((hold_x, "hold_x"), (hold_y, "hold_y")):
+        if f is not None:
+            _fmt(f, name)
+    with _On(x, stream) as s:
+        y = torch.empty((m, w), dtype=dtype, device=dev)
+        d.y, d.ldy = y.data_ptr(), w
+        out = [y]
+        if stats:
+            st = torch.empty((2, m), dtype=torch.float32, device=dev)
+            d.stats = st.data_ptr()
+            out.append(st)
+        if hold_x is not None:
+            h = Held.empty(m, w, hold_x, dtype, dev)
+            d.x_hold, d.xq, d.x_scale = HOLDS[hold_x], h.q.data_ptr(), h.scale.data_ptr()
+            out.append(h)
+        if hold_y is not None:
+            h = Held.empty(m, w, hold_y, dtype, dev)
+            d.y_hold, d.yq, d.y_scale = HOLDS[hold_y], h.q.data_ptr(), h.scale.data_ptr()
+            out.append(h)
+        _check(lib().nr_layer_norm(C.byref(d), s), "nr_layer_norm")
+    return out[0] if len(out) == 1 else tuple(out)
+
+
+def nr_layer_norm_grad(dy: torch.Tensor, x, stats: torch.Tensor,
+                       weight: Optional[torch.Tensor] = None, add: Optional[torch.Tensor] = None,
+                       dx: bool = True, dweight: bool = True, dbias: bool = True, stream=None):
+    """(dx, dweight, dbias) of nr_layer_norm, None for those not asked for; `add`
+    (the gradient that reaches x on another path) is added to dx.  x may be Held."""
+    dtype, dev = _layer_input(dy, "dy")
+    m, w = dy.shape
+    d = nr_layer_norm_grad_desc()
+    d.m, d.d, d.dtype = m, w, LAYER_DTYPES[dtype]
+    d.dy, d.lddy = _mat(dy, "dy", dtype, dev)
+    if isinstance(x, Held):
+        d.x, d.ldx, d.x_hold, d.x_scale = _held(x, "x", dtype, dev, m, w)
+    else:
+        d.x, d.ldx = _mat(x, "x", dtype, dev, m, w)
+    _fits(stats, "stats", torch.float32, 2, m)
+    if stats.device != dev:
+        raise ValueError(f"stats must be on {dev}")
+    d.stats = stats.data_ptr()
+    d.weight = _vec(weight, "weight", dtype, dev, w)
+    if add is not None:
+        d.add, d.ldadd = _mat(add, "add", dtype, dev, m, w)
+    with _On(dy, stream) as s:
+        gx = torch.empty((m, w), dtype=dtype, device=dev) if dx else None
+        gw = torch.empty(w, dtype=dtype, device=dev) if dweight else None
+        gb = torch.empty(w, dtype=dtype, device=dev) if dbias else None
+        if dx:
+            d.dx, d.lddx = gx.data_ptr(), w
+        if dweight:
+            d.dweight = gw.data_ptr()
+        if dbias:
+            d.dbias = gb.data_ptr()
+        L = lib()
+        nb = L.nr_layer_norm_grad_ws(C.byref(d))
+        ws = _work(nb, dev)
+        _check(L.nr_layer_norm_grad(C.byref(d), None if ws is None else ws.data_ptr(), nb, s),
+               "nr_layer_norm_grad")
+    return gx, gw, gb
 
 
 # --------------------------------------------------------------------------
