@@ -5,11 +5,10 @@
 //   y   i = row, j = output, k = input:   both operands have k along their rows
 //   dx  i = row, j = input, k = output:   w has j along its rows
 //   dw  i = output, j = input, k = row:   both have i or j along their rows
-// A block of 256 threads owns a 64 x 64 tile, each wave a 32 x 32 quarter, in
-// blocks of 16 x 16 of the fp32 matrix cores.  j takes the place of the
-// instruction's rows, so that a lane holds four neighbouring elements of a row
-// of the output.  Where the tiles are few and k long, k is cut and the parts'
-// fp32 sums are added in order by a second kernel with the same epilogue.
+// j takes the place of the matrix instruction's rows, so that a lane holds four
+// neighbouring elements of a row of the output.  Where the tiles are few and k
+// long, k is cut and the parts' fp32 sums are added in order by a second kernel
+// with the same epilogue.
 #include "nr_layers.h"
 
 namespace nr {
@@ -119,94 +118,284 @@ __device__ __forceinline__ void finish(const GemmArgs &a, int64_t i, int j0, boo
   }
 }
 
-constexpr int GT = 64, GK = 16;
+// ---------------------------------------------------------------- the tiles
+//
+// The 16-bit types go to the matrix cores as they are; a float goes as three
+// bf16 (its upper eight significant bits, the next eight, and the rest), and a
+// product of two floats as the six products of parts that are above 2^-24 of
+// it.  The matrix cores make 16 bf16 products in the time of one fp32 product,
+// so six still leave 2.7 times the rate, and what is dropped is of the size of
+// the rounding that an fp32 product has anyway.
+template <class T>
+struct Tile {
+  typedef T E;
+  static constexpr int P = 1, BK = 64, NBUF = 2;
+};
+template <>
+struct Tile<float> {
+  typedef bf16_t E;
+  static constexpr int P = 3, BK = 32, NBUF = 1;
+};
 
-// four elements (along the operand's rows) of a K-tile: where k runs along the
-// rows, row `o` of the tile's side and k0..; otherwise row k and columns o..
-template <class T, bool KC, bool HELD>
-__device__ __forceinline__ void stage4(const LayerMat &m, int64_t o, int64_t nO, int64_t k,
-                                       int64_t kend, float (&v)[4]) {
-  const int64_t row = KC ? o : k, rows = KC ? nO : kend;
-  const int64_t col = KC ? k : o, cols = KC ? kend : nO;
-#pragma unroll
-  for (int r = 0; r < 4; ++r) v[r] = 0.0f;
-  if (row >= rows) return;
-  if constexpr (HELD) {
-    if (col < cols) {
-      hold_unpack4(*reinterpret_cast<const uint32_t *>((const uint8_t *)m.p + row * m.ld + col),
-                   hold_scale(m.scale[row * (m.ld / 32) + col / 32]), m.hold, v);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) v[r] = to_f32(from_f32<T>(v[r]));
-    }
-  } else {
-    const T *p = (const T *)m.p + row * m.ld + col;
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      if (col + r < cols) v[r] = to_f32(p[r]);
-  }
+typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
+typedef f16_t f16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+__device__ __forceinline__ v4f mma(bf16x8 a, bf16x8 b, v4f c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ v4f mma(f16x8 a, f16x8 b, v4f c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
-template <class T, bool IK, bool JK, bool HELD, bool LIN>
-__global__ void __launch_bounds__(256) k_gemm(GemmArgs a) {
-  __shared__ float As[GK][GT + 4], Bs[GK][GT + 4];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int wi = 32 * (wave & 1), wj = 32 * (wave >> 1);
-  const int64_t tj = (a.J + GT - 1) / GT, tiles = (a.I + GT - 1) / GT * tj;
-  const int64_t k0 = (int64_t)blockIdx.y * a.kchunk;
-  const int64_t k1 = k0 + a.kchunk < a.K ? k0 + a.kchunk : a.K;
-  for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
-    const int64_t i0 = t / tj * GT;
-    const int j0 = (int)(t % tj) * GT;
-    v4f acc[2][2];   // [i][j]
+// One operand's K-tile: BK of k by R of its side, in chunks of eight elements
+// (16 bytes of LDS), read from memory into registers and, a K-tile later, put
+// into LDS.
+//   KC (k along the operand's rows): [R][BK]; the chunks of a row are exchanged
+//     by the row's number, so that the sixteen rows that a matrix instruction
+//     reads at one k lie on different banks.
+//   otherwise: [BK][R]; pairs of chunks (the sixteen columns of a block) are
+//     exchanged by k, and a block is read transposed (ds_read_b64_tr_b16: sixteen
+//     lanes give the addresses of four rows of sixteen columns, and lane t
+//     receives the four elements of column t).
+template <class T, int R, bool KC, bool HELD>
+struct Operand {
+  typedef typename Tile<T>::E E;
+  typedef E E8 __attribute__((ext_vector_type(8)));
+  static constexpr int BK = Tile<T>::BK, P = Tile<T>::P;
+  static constexpr int N = R * BK / 8 / 256;      // chunks per thread
+  static constexpr int CPR = (KC ? BK : R) / 8;   // chunks per row of the tile in memory
+  static constexpr int PLANE = R * BK * 2, BYTES = P * PLANE;
+  static_assert(N >= 1 && N * 256 * 8 == R * BK, "whole chunks per thread");
+
+  uint4 raw[N][sizeof(T) / 2];   // what the thread has read; of held rows:
+  uint2 q[N];
+  uint32_t scale[N];
+
+  static __device__ __forceinline__ int slot(int row, int c) {
+    if constexpr (KC && BK == 64) return row * CPR + (c ^ (row & 7));
+    else if constexpr (KC)
+      return row * CPR + (c ^ (((row >> 2) & 1) | ((((row >> 1) ^ (row >> 3)) & 1) << 1)));
+    else if constexpr (R == 128) return row * CPR + (c ^ (((row & 3) | ((row >> 3) & 1) << 2) << 1));
+    else return row * CPR + (c ^ ((row & 3) << 1));
+  }
+
+  // [o0, o0 + R) x [k, k + BK).  Past kend, and past nO where the side runs along
+  // the rows, zeros; rows of a KC operand past nO repeat the last (their outputs
+  // are dropped).  FULL: nothing is past an end
+  template <bool FULL>
+  __device__ __forceinline__ void fetch(const LayerMat &m, int64_t o0, int64_t nO, int64_t k,
+                                        int64_t kend) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int u = 0; u < N; ++u) {
+      const int e = threadIdx.x + 256 * u;
+      int64_t row = (KC ? o0 : k) + e / CPR;
+      const int64_t col = (KC ? k : o0) + 8 * (e % CPR), cols = KC ? kend : nO;
+      bool in = true;
+      if constexpr (!FULL && KC) row = row < nO ? row : nO - 1;
+      if constexpr (!FULL && !KC) in = row < kend;
+      if constexpr (HELD) {
+        q[u] = make_uint2(0, 0);
+        scale[u] = 127;
+        if (FULL || (in && col < m.ld)) {   // padded to whole groups, zeros behind the width
+          q[u] = *reinterpret_cast<const uint2 *>((const uint8_t *)m.p + row * m.ld + col);
+          scale[u] = m.scale[row * (m.ld / 32) + col / 32];
+        }
+      } else {
+        const T *p = (const T *)m.p + row * m.ld + col;
+        if (FULL || (in && col + 8 <= cols)) {
+          __builtin_memcpy(raw[u], p, 8 * sizeof(T));   // any alignment of the element
+        } else {
+          T v[8];
 #pragma unroll
-      for (int j = 0; j < 2; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
-    for (int64_t k = k0; k < k1; k += GK) {
-      float va[4], vb[4];
-      const int oi = IK ? tid / 4 : 4 * (tid % 16), ki = IK ? 4 * (tid % 4) : tid / 16;
-      const int oj = JK ? tid / 4 : 4 * (tid % 16), kj = JK ? 4 * (tid % 4) : tid / 16;
-      stage4<T, IK, false>(a.A, i0 + oi, a.I, k + ki, k1, va);
-      stage4<T, JK, HELD>(a.B, j0 + oj, a.J, k + kj, k1, vb);
-      __syncthreads();
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        As[IK ? ki + r : ki][IK ? oi : oi + r] = va[r];
-        Bs[JK ? kj + r : kj][JK ? oj : oj + r] = vb[r];
+          for (int i = 0; i < 8; ++i) v[i] = in && col + i < cols ? p[i] : (T)0.0f;
+          __builtin_memcpy(raw[u], v, 8 * sizeof(T));
+        }
       }
-      __syncthreads();
+    }
+  }
+
+  __device__ __forceinline__ void stash(char *lds, int hold) const {
 #pragma unroll
-      for (int kk = 0; kk < GK; kk += 4) {
-        const int kr = kk + (lane >> 4), c = lane & 15;
-        float av[2], bv[2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          av[u] = As[kr][wi + 16 * u + c];
-          bv[u] = Bs[kr][wj + 16 * u + c];
+    for (int u = 0; u < N; ++u) {
+      const int e = threadIdx.x + 256 * u;
+      char *at = lds + slot(e / CPR, e % CPR) * 16;
+      if constexpr (sizeof(T) == 2 && !HELD) {
+        *reinterpret_cast<uint4 *>(at) = raw[u][0];
+      } else {
+        float v[8];
+        if constexpr (HELD) {
+          const float s = hold_scale((uint8_t)scale[u]);
+          hold_unpack4(q[u].x, s, hold, v);
+          hold_unpack4(q[u].y, s, hold, v + 4);
+        } else {
+          __builtin_memcpy(v, raw[u], 32);
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int p = 0; p < P; ++p) {   // each part is the rest, rounded to nearest
+          E8 o;
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(bv[j], av[i], acc[i][j], 0, 0, 0);
+          for (int i = 0; i < 8; ++i) {
+            o[i] = from_f32<E>(v[i]);
+            if (p + 1 < P) v[i] -= to_f32(o[i]);
+          }
+          *reinterpret_cast<E8 *>(at + p * PLANE) = o;
+        }
+      }
+    }
+  }
+
+  // of a 16 x 16 x 32 block from b0 of the side and k = 32 s on: lane l has side
+  // b0 + l % 16, k = 32 s + 8 (l / 16) and the seven after it
+  static __device__ __forceinline__ E8 frag(const char *lds, int p, int b0, int s) {
+    const int t = lane_id() & 15, g = lane_id() >> 4;
+    lds += p * PLANE;
+    if constexpr (KC) {
+      return *reinterpret_cast<const E8 *>(lds + slot(b0 + t, 4 * s + g) * 16);
+    } else {
+      typedef __attribute__((address_space(3))) s16x4 lds4;
+      const int k = 32 * s + 8 * g + (t >> 2), c = b0 / 8 + ((t & 3) >> 1), in = 8 * (t & 1);
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(lds + slot(k, c) * 16 + in));
+      const s16x4 hi =
+          __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(lds + slot(k + 4, c) * 16 + in));
+      return __builtin_bit_cast(E8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+  }
+};
+
+// One output as a plain chain of fp32, for those that came out infinite or as no
+// number: the parts of an infinity (or of a float above the largest bf16) make
+// NaN of what is an infinity or a number
+template <bool IK, bool JK, bool HELD>
+__device__ __noinline__ float plain_chain(const GemmArgs &a, int64_t i, int j, int64_t k0,
+                                          int64_t k1) {
+  float s = 0.0f;
+  for (int64_t k = k0; k < k1; ++k) {
+    const float x = ((const float *)a.A.p)[IK ? i * a.A.ld + k : k * a.A.ld + i];
+    float w;
+    if constexpr (HELD) {
+      float v[4];
+      const uint8_t b = ((const uint8_t *)a.B.p)[k * a.B.ld + j];
+      hold_unpack4(b, hold_scale(a.B.scale[k * (a.B.ld / 32) + j / 32]), a.B.hold, v);
+      w = v[0];
+    } else {
+      w = ((const float *)a.B.p)[JK ? j * a.B.ld + k : k * a.B.ld + j];
+    }
+    s = fmaf(x, w, s);
+  }
+  return s;
+}
+
+// A block of 256 threads owns a TI x TJ tile, each wave a quarter of it in
+// blocks of 16 x 16.  The next K-tile is read into registers while this one is
+// multiplied.  Blocks go to the eight XCDs in turn: each XCD takes a run of
+// neighbouring tiles, so that their operands meet in its L2.
+template <class T, int TI, int TJ, bool IK, bool JK, bool HELD, bool LIN>
+__global__ void __launch_bounds__(256) k_gemm(GemmArgs a) {
+  typedef Operand<T, TI, IK, false> OA;
+  typedef Operand<T, TJ, JK, HELD> OB;
+  typedef typename OA::E8 E8;
+  constexpr int BK = OA::BK, P = OA::P, NBUF = Tile<T>::NBUF;
+  constexpr int NI = TI / 32, NJ = TJ / 32;
+  __shared__ __attribute__((aligned(16))) char lds[NBUF][OA::BYTES + OB::BYTES];
+  const int lane = lane_id(), wave = threadIdx.x / WAVE;
+  const int wi = TI / 2 * (wave & 1), wj = TJ / 2 * (wave >> 1);
+  const int64_t tj = (a.J + TJ - 1) / TJ, tiles = (a.I + TI - 1) / TI * tj;
+  const int64_t per = (tiles + 7) / 8;
+  const int64_t k0 = (int64_t)blockIdx.y * a.kchunk;
+  const int64_t k1 = k0 + a.kchunk < a.K ? k0 + a.kchunk : a.K;
+  for (int64_t u = blockIdx.x; u < 8 * per; u += gridDim.x) {
+    const int64_t t = (u & 7) * per + (u >> 3);
+    if (t >= tiles) continue;   // the whole block together
+    const int64_t i0 = t / tj * TI, j0 = t % tj * TJ;
+    const bool inside = i0 + TI <= a.I && j0 + TJ <= a.J;
+    OA fa;
+    OB fb;
+    auto fetch = [&](int64_t k) {
+      if (inside && k + BK <= k1) {
+        fa.template fetch<true>(a.A, i0, a.I, k, k1);
+        fb.template fetch<true>(a.B, j0, a.J, k, k1);
+      } else {
+        fa.template fetch<false>(a.A, i0, a.I, k, k1);
+        fb.template fetch<false>(a.B, j0, a.J, k, k1);
+      }
+    };
+    auto stash = [&](int buf) {
+      fa.stash(lds[buf], 0);
+      fb.stash(lds[buf] + OA::BYTES, a.B.hold);
+    };
+    v4f acc[NI][NJ];
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
+    int buf = 0;
+    if (k0 < k1) {
+      fetch(k0);
+      __syncthreads();   // the tile before has been read
+      stash(0);
+      __syncthreads();
+    }
+    for (int64_t k = k0; k < k1; k += BK) {
+      const bool more = k + BK < k1;
+      if (more) fetch(k + BK);
+#pragma unroll
+      for (int s = 0; s < BK / 32; ++s) {
+        E8 fi[P][NI], fj[P][NJ];
+#pragma unroll
+        for (int p = 0; p < P; ++p) {
+#pragma unroll
+          for (int i = 0; i < NI; ++i) fi[p][i] = OA::frag(lds[buf], p, wi + 16 * i, s);
+#pragma unroll
+          for (int j = 0; j < NJ; ++j)
+            fj[p][j] = OB::frag(lds[buf] + OA::BYTES, p, wj + 16 * j, s);
+        }
+#pragma unroll
+        for (int q = P - 1; q >= 0; --q)       // the small products first
+#pragma unroll
+          for (int p = 0; p <= q; ++p)
+#pragma unroll
+            for (int i = 0; i < NI; ++i)
+#pragma unroll
+              for (int j = 0; j < NJ; ++j) acc[i][j] = mma(fj[q - p][j], fi[p][i], acc[i][j]);
+      }
+      if (NBUF == 1) __syncthreads();
+      if (more) {
+        if (NBUF == 2) buf ^= 1;
+        stash(buf);
+        __syncthreads();
       }
     }
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < NI; ++i) {
       const int64_t row = i0 + wi + 16 * i + (lane & 15);
-      float v[2][4];
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
+      for (int j2 = 0; j2 < NJ; j2 += 2) {
+        const int64_t c0 = j0 + wj + 16 * j2;
+        if (c0 >= a.J) continue;   // the whole wave together
+        float v[2][4];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) v[j][r] = acc[i][j][r];
-      if (a.part) {
-        float *p = a.part + ((int64_t)blockIdx.y * a.I + row) * a.ldp + j0 + wj + 4 * (lane >> 4);
+        for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-          if (row < a.I && j0 + wj < a.ldp)
-            *reinterpret_cast<float4 *>(p + 16 * j) = make_float4(v[j][0], v[j][1], v[j][2], v[j][3]);
-      } else {
-        finish<T, LIN>(a, row, j0 + wj, row < a.I, v);
+          for (int r = 0; r < 4; ++r) {
+            v[b][r] = acc[i][j2 + b][r];
+            if constexpr (P == 3) {
+              const int64_t c = c0 + 16 * b + 4 * (lane >> 4) + r;
+              if (!(fabsf(v[b][r]) < INFINITY) && row < a.I && c < a.J)
+                v[b][r] = plain_chain<IK, JK, HELD>(a, row, (int)c, k0, k1);
+            }
+          }
+        if (a.part) {
+          float *o = a.part + ((int64_t)blockIdx.y * a.I + row) * a.ldp + c0 + 4 * (lane >> 4);
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+            if (row < a.I)
+              *reinterpret_cast<float4 *>(o + 16 * b) =
+                  make_float4(v[b][0], v[b][1], v[b][2], v[b][3]);
+        } else {
+          finish<T, LIN>(a, row, (int)c0, row < a.I, v);
+        }
       }
     }
   }
@@ -284,23 +473,41 @@ static bool aligned(const void *p, int64_t ld, size_t e, size_t to) {
   return !p || (reinterpret_cast<uintptr_t>(p) % to == 0 && ld * e % to == 0);
 }
 
+// How a product is cut: the tile's side, and parts of k.  128 x 128 tiles read
+// half of what 64 x 64 ones do, if there are enough of them to go round
 struct Split {
-  int parts;
+  int side, parts;
   int64_t kchunk;
 };
-// Parts of k: enough for two blocks per CU, each of at least 128 of k
 static Split split_of(int64_t I, int J, int64_t K) {
-  const int64_t tiles = up(I, GT) / GT * (up(J, GT) / GT);
-  int64_t parts = tiles > 0 ? (512 + tiles - 1) / tiles : 1;
-  const int64_t most = K / 128 < 64 ? K / 128 : 64;
-  if (tiles >= 256 || most < 2) parts = 1;
-  else if (parts > most) parts = most;
-  const int64_t kc = up((K + parts - 1) / parts, GK);
-  return {K > 0 ? (int)((K + kc - 1) / kc) : 1, kc > 0 ? kc : GK};
+  auto tiles = [&](int64_t t) { return up(I, t) / t * (up(J, t) / t); };
+  Split sp{128, 1, 64};
+  if (tiles(128) < 256 && tiles(128) * (K / 512) < 256) sp.side = 64;
+  const int64_t n = tiles(sp.side);
+  int64_t parts = n > 0 && n < 256 ? (512 + n - 1) / n : 1;
+  const int64_t most = K / 256 < 64 ? K / 256 : 64;
+  if (parts > most) parts = most;
+  if (parts < 2) parts = 1;
+  sp.kchunk = K > 0 ? up((K + parts - 1) / parts, 64) : 64;
+  sp.parts = K > 0 ? (int)((K + sp.kchunk - 1) / sp.kchunk) : 1;
+  return sp;
 }
 static size_t part_bytes(int64_t I, int J, int64_t K) {
   const Split sp = split_of(I, J, K);
   return sp.parts > 1 ? sizeof(float) * (size_t)sp.parts * I * up(J, 32) : 0;
+}
+
+template <class T, int S, bool IK, bool JK, bool LIN>
+static void gemm_tiles(const GemmArgs &a, int parts, hipStream_t s) {
+  const int64_t tiles = up(up(a.I, S) / S * (up(a.J, S) / S), 8);
+  const dim3 g((unsigned)(tiles < 1 << 22 ? tiles : 1 << 22), parts);
+  if constexpr (!IK) {
+    if (a.B.hold) {
+      hipLaunchKernelGGL((k_gemm<T, S, S, IK, JK, true, LIN>), g, dim3(256), 0, s, a);
+      return;
+    }
+  }
+  hipLaunchKernelGGL((k_gemm<T, S, S, IK, JK, false, LIN>), g, dim3(256), 0, s, a);
 }
 
 template <class T, bool IK, bool JK, bool LIN>
@@ -310,16 +517,8 @@ static hipError_t gemm(GemmArgs a, float *ws, hipStream_t s) {
   a.kchunk = sp.kchunk;
   a.part = sp.parts > 1 ? ws : nullptr;
   a.ldp = up(a.J, 32);
-  const int64_t tiles = up(a.I, GT) / GT * (up(a.J, GT) / GT);
-  const dim3 g((unsigned)(tiles < 1 << 22 ? tiles : 1 << 22), sp.parts);
-  if constexpr (!JK) {
-    if (a.B.hold)
-      hipLaunchKernelGGL((k_gemm<T, IK, JK, true, LIN>), g, dim3(256), 0, s, a);
-    else
-      hipLaunchKernelGGL((k_gemm<T, IK, JK, false, LIN>), g, dim3(256), 0, s, a);
-  } else {
-    hipLaunchKernelGGL((k_gemm<T, IK, JK, false, LIN>), g, dim3(256), 0, s, a);
-  }
+  if (sp.side == 128) gemm_tiles<T, 128, IK, JK, LIN>(a, sp.parts, s);
+  else gemm_tiles<T, 64, IK, JK, LIN>(a, sp.parts, s);
   if (sp.parts > 1) {
     const int64_t blocks = (up(a.I, 16) / 16 * (up(a.J, 32) / 32) + 3) / 4;
     hipLaunchKernelGGL((k_gemm_join<T, LIN>), dim3((unsigned)(blocks < 1 << 20 ? blocks : 1 << 20)),
