@@ -7,7 +7,7 @@
 
 namespace nr {
 
-template <class T, bool VEC>
+template <class T>
 __global__ void __launch_bounds__(256) k_act_hold(const T *x, int64_t ldx, int64_t m, int d,
                                                   int hold, uint8_t *q, uint8_t *scale) {
   const int64_t ldq = (d + 31) / 32 * 32;
@@ -17,13 +17,13 @@ __global__ void __launch_bounds__(256) k_act_hold(const T *x, int64_t ldx, int64
     const int64_t row = u / (ldq / 8);
     const int c0 = (int)(u - row * (ldq / 8)) * 8;
     float v[8];
-    load8<T, VEC>(x + row * ldx, c0, d, v);
+    load8(x + row * ldx, c0, d, v);
     write8(q + row * ldq, scale + row * (ldq / 32), c0, hold, __is_same(T, f16_t),
            v);
   }
 }
 
-template <class T, bool VEC>
+template <class T>
 __global__ void __launch_bounds__(256) k_act_read(const uint8_t *q, const uint8_t *scale,
                                                   int64_t m, int d, int hold, T *y, int64_t ldy) {
   const int64_t ldq = (d + 31) / 32 * 32;
@@ -33,7 +33,7 @@ __global__ void __launch_bounds__(256) k_act_read(const uint8_t *q, const uint8_
     const int c0 = (int)(u - row * (ldq / 8)) * 8;
     float v[8];
     read8<T>(q + row * ldq, scale + row * (ldq / 32), c0, hold, v);
-    store8<T, VEC>(y + row * ldy, c0, d, v);
+    store8(y + row * ldy, c0, d, v);
   }
 }
 
@@ -45,9 +45,7 @@ static unsigned hold_grid(int64_t m, int d) {
 template <class T>
 static hipError_t hold_t(const void *x, int64_t ldx, int64_t m, int d, int hold, uint8_t *q,
                          uint8_t *scale, hipStream_t s) {
-  const bool vec = reinterpret_cast<uintptr_t>(x) % 16 == 0 && ldx * sizeof(T) % 16 == 0;
-  const auto f = vec ? k_act_hold<T, true> : k_act_hold<T, false>;
-  hipLaunchKernelGGL(f, dim3(hold_grid(m, d)), dim3(256), 0, s, (const T *)x, ldx, m, d, hold, q,
+  hipLaunchKernelGGL(k_act_hold<T>, dim3(hold_grid(m, d)), dim3(256), 0, s, (const T *)x, ldx, m, d, hold, q,
                      scale);
   return hipGetLastError();
 }
@@ -55,9 +53,7 @@ static hipError_t hold_t(const void *x, int64_t ldx, int64_t m, int d, int hold,
 template <class T>
 static hipError_t read_t(const uint8_t *q, const uint8_t *scale, int64_t m, int d, int hold,
                          void *y, int64_t ldy, hipStream_t s) {
-  const bool vec = reinterpret_cast<uintptr_t>(y) % 16 == 0 && ldy * sizeof(T) % 16 == 0;
-  const auto f = vec ? k_act_read<T, true> : k_act_read<T, false>;
-  hipLaunchKernelGGL(f, dim3(hold_grid(m, d)), dim3(256), 0, s, q, scale, m, d, hold, (T *)y, ldy);
+  hipLaunchKernelGGL(k_act_read<T>, dim3(hold_grid(m, d)), dim3(256), 0, s, q, scale, m, d, hold, (T *)y, ldy);
   return hipGetLastError();
 }
 

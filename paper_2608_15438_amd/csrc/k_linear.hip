@@ -21,100 +21,46 @@ struct GemmArgs {
   LayerMat A, B;         // B may be held in 8 bits where j runs along its rows
   float *part;           // [parts][I][ldp] sums of the parts, or NULL
   int64_t ldp;
-  int vec;               // outputs (and residual) can be accessed four elements at a time
   void *out;             // without the layer's epilogue: [I][ldo]
   int64_t ldo;
   LinearArgs lin;
 };
 
-template <class T>
-__device__ __forceinline__ void store4(T *p, const float (&v)[4], int n, bool vec) {
-  if (vec && n >= 4) {
-    typedef T t4 __attribute__((ext_vector_type(4)));
-    t4 o;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) o[r] = from_f32<T>(v[r]);
-    *reinterpret_cast<t4 *>(p) = o;
-  } else {
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      if (r < n) p[r] = from_f32<T>(v[r]);
-  }
-}
-
-template <class T>
-__device__ __forceinline__ void load4(const T *p, float (&v)[4], int n, bool vec) {
-  if (vec && n >= 4) {
-    typedef T t4 __attribute__((ext_vector_type(4)));
-    const t4 o = *reinterpret_cast<const t4 *>(p);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] = to_f32(o[r]);
-  } else {
-#pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] = r < n ? to_f32(p[r]) : 0.0f;
-  }
-}
-
-// The epilogue of 16 rows x 32 columns in a wave: lane l holds row l % 16,
-// columns j0 + 16 b + 4 (l / 16) + r.  The whole wave calls it together (a
-// group held in 8 bits lies in four lanes); ok: the lane's row is inside
+// The epilogue of eight columns of a row from j on (a multiple of 8).  A group held
+// in 8 bits lies in the lanes of a quad, which call it together; ok: the row is
+// inside
 template <class T, bool LIN>
-__device__ __forceinline__ void finish(const GemmArgs &a, int64_t i, int j0, bool ok,
-                                       float (&v)[2][4]) {
-  constexpr bool exact = sizeof(T) == 4;
-  const int c = j0 + 4 * (lane_id() >> 4);
+__device__ __forceinline__ void finish(const GemmArgs &a, int64_t i, int j, bool ok,
+                                       float (&v)[8]) {
   if constexpr (!LIN) {
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-      if (ok && c + 16 * b < a.J)
-        store4((T *)a.out + i * a.ldo + c + 16 * b, v[b], a.J - c - 16 * b, a.vec);
+    if (ok) store8((T *)a.out + i * a.ldo, j, a.J, v);
   } else {
+    constexpr bool exact = sizeof(T) == 4;
     const LinearArgs &l = a.lin;
+    float u[8];
     if (l.bias) {
+      load8((const T *)l.bias, j, a.J, u);
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int j = c + 16 * b + r;
-          if (j < a.J) v[b][r] += to_f32(((const T *)l.bias)[j]);
-        }
+      for (int r = 0; r < 8; ++r) v[r] += u[r];
     }
     if (l.pre_hold) {
-      float z[2][4];
-      uint32_t m = 0;
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          z[b][r] = c + 16 * b + r < a.J ? to_f32(from_f32<T>(v[b][r])) : 0.0f;
-          const uint32_t u = __float_as_uint(z[b][r]) & 0x7fffffffu;
-          m = m > u ? m : u;
-        }
-      uint32_t o = xor_lane<16>(m);
-      m = m > o ? m : o;
-      o = xor_lane<32>(m);
-      m = m > o ? m : o;
-      const int byte = hold_byte(m, l.pre_hold, __is_same(T, f16_t));
-      if (ok && j0 < a.J) {
-        uint8_t *q = (uint8_t *)l.pre + i * l.ldp + c;
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-          *reinterpret_cast<uint32_t *>(q + 16 * b) =
-              hold_pack4(z[b][0], z[b][1], z[b][2], z[b][3], byte, l.pre_hold);
-        if (lane_id() < 16) l.pre_scale[i * (l.ldp / 32) + j0 / 32] = (uint8_t)byte;
-      }
+      for (int r = 0; r < 8; ++r) u[r] = j + r < a.J ? to_f32(from_f32<T>(v[r])) : 0.0f;
+      if (ok && j < l.ldp)   // the rows of q are whole groups, so a quad is in or out
+        write8((uint8_t *)l.pre + i * l.ldp, l.pre_scale + i * (l.ldp / 32), j, l.pre_hold,
+               __is_same(T, f16_t), u);
+    } else if (l.pre && ok) {
+      store8((T *)l.pre + i * l.ldp, j, a.J, v);
     }
+    if (!ok) return;
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const int cb = c + 16 * b, n = a.J - cb;
-      if (!ok || n <= 0) continue;
-      if (l.pre && !l.pre_hold) store4((T *)l.pre + i * l.ldp + cb, v[b], n, a.vec);
-      float s[4] = {};
-      if (l.res) load4((const T *)l.res + i * l.ldr + cb, s, n, a.vec);
+    for (int r = 0; r < 8; ++r) v[r] = act_value<exact>(v[r], l.act);
+    if (l.res) {
+      load8((const T *)l.res + i * l.ldr, j, a.J, u);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) s[r] += act_value<exact>(v[b][r], l.act);
-      store4((T *)l.y + i * l.ldy + cb, s, n, a.vec);
+      for (int r = 0; r < 8; ++r) v[r] += u[r];
     }
+    store8((T *)l.y + i * l.ldy, j, a.J, v);
   }
 }
 
@@ -149,6 +95,8 @@ __device__ __forceinline__ v4f mma(f16x8 a, f16x8 b, v4f c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
+__device__ const uint4 zero_chunk = {0, 0, 0, 0};
+
 // One operand's K-tile: BK of k by R of its side, in chunks of eight elements
 // (16 bytes of LDS), read from memory into registers and, a K-tile later, put
 // into LDS.
@@ -159,27 +107,29 @@ __device__ __forceinline__ v4f mma(f16x8 a, f16x8 b, v4f c) {
 //     exchanged by k, and a block is read transposed (ds_read_b64_tr_b16: sixteen
 //     lanes give the addresses of four rows of sixteen columns, and lane t
 //     receives the four elements of column t).
-template <class T, int R, bool KC, bool HELD>
+template <class T, int R, bool KC, bool HELD, int NT = 256>
 struct Operand {
   typedef typename Tile<T>::E E;
   typedef E E8 __attribute__((ext_vector_type(8)));
   static constexpr int BK = Tile<T>::BK, P = Tile<T>::P;
-  static constexpr int N = R * BK / 8 / 256;      // chunks per thread
+  static constexpr int N = R * BK / 8 / NT;       // chunks per thread
   static constexpr int CPR = (KC ? BK : R) / 8;   // chunks per row of the tile in memory
   static constexpr int PLANE = R * BK * 2, BYTES = P * PLANE;
-  static_assert(N >= 1 && N * 256 * 8 == R * BK, "whole chunks per thread");
+  static_assert(N >= 1 && N * NT * 8 == R * BK, "whole chunks per thread");
 
   uint4 raw[N][sizeof(T) / 2];   // what the thread has read; of held rows:
   uint2 q[N];
   uint32_t scale[N];
 
-  static __device__ __forceinline__ int slot(int row, int c) {
-    if constexpr (KC && BK == 64) return row * CPR + (c ^ (row & 7));
-    else if constexpr (KC)
-      return row * CPR + (c ^ (((row >> 2) & 1) | ((((row >> 1) ^ (row >> 3)) & 1) << 1)));
-    else if constexpr (R == 128) return row * CPR + (c ^ (((row & 3) | ((row >> 3) & 1) << 2) << 1));
-    else return row * CPR + (c ^ ((row & 3) << 1));
+  // where chunk c of a row lies, and (the exchange being its own inverse) the
+  // chunk that lies at place c
+  static __device__ __forceinline__ int swap(int row, int c) {
+    if constexpr (KC && BK == 64) return c ^ (row & 7);
+    else if constexpr (KC) return c ^ (((row >> 2) & 1) | ((((row >> 1) ^ (row >> 3)) & 1) << 1));
+    else if constexpr (R >= 128) return c ^ (((row & 3) | ((row >> 3) & 1) << 2) << 1);
+    else return c ^ ((row & 3) << 1);
   }
+  static __device__ __forceinline__ int slot(int row, int c) { return row * CPR + swap(row, c); }
 
   // [o0, o0 + R) x [k, k + BK).  Past kend, and past nO where the side runs along
   // the rows, zeros; rows of a KC operand past nO repeat the last (their outputs
@@ -189,7 +139,7 @@ struct Operand {
                                         int64_t kend) {
 #pragma unroll
     for (int u = 0; u < N; ++u) {
-      const int e = threadIdx.x + 256 * u;
+      const int e = threadIdx.x + NT * u;
       int64_t row = (KC ? o0 : k) + e / CPR;
       const int64_t col = (KC ? k : o0) + 8 * (e % CPR), cols = KC ? kend : nO;
       bool in = true;
@@ -219,7 +169,7 @@ struct Operand {
   __device__ __forceinline__ void stash(char *lds, int hold) const {
 #pragma unroll
     for (int u = 0; u < N; ++u) {
-      const int e = threadIdx.x + 256 * u;
+      const int e = threadIdx.x + NT * u;
       char *at = lds + slot(e / CPR, e % CPR) * 16;
       if constexpr (sizeof(T) == 2 && !HELD) {
         *reinterpret_cast<uint4 *>(at) = raw[u][0];
@@ -246,10 +196,45 @@ struct Operand {
     }
   }
 
+  // The same straight from memory into LDS, for rows that lie on 16-byte
+  // boundaries and whole chunks: a wave's 64 chunks go to 1 KB in a row, so each
+  // lane reads the chunk that belongs in its place.  offset: the lane's bytes
+  // from the tile's first element, found once; a side past nO repeats its last
+  // row or chunk (outputs that are dropped)
+  static __device__ __forceinline__ void dma_offsets(const LayerMat &m, int64_t o0, int64_t nO,
+                                                     uint32_t (&offset)[N]) {
+    const int64_t left = nO - o0;
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const int e = threadIdx.x + NT * u;
+      int row = e / CPR, c = swap(row, e % CPR);
+      if (KC) row = row < left ? row : (int)left - 1;
+      else c = 8 * c < left ? c : (int)(left / 8) - 1;
+      offset[u] = (uint32_t)(row * m.ld + 8 * c) * (uint32_t)sizeof(T);
+    }
+  }
+  // k of the chunks within the tile from `left` on: zeros
+  template <bool FULL>
+  static __device__ __forceinline__ void dma(const T *base, const uint32_t (&offset)[N], char *lds,
+                                             int left) {
+    typedef __attribute__((address_space(1))) const char *global_t;
+    typedef __attribute__((address_space(3))) char *lds_t;
+    lds += threadIdx.x / WAVE * 1024;
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const char *p = (const char *)base + offset[u];
+      if constexpr (!FULL) {
+        const int e = threadIdx.x + NT * u;
+        if ((KC ? 8 * swap(e / CPR, e % CPR) : e / CPR) >= left) p = (const char *)&zero_chunk;
+      }
+      __builtin_amdgcn_global_load_lds((global_t)p, (lds_t)(lds + NT * 16 * u), 16, 0, 0);
+    }
+  }
+
   // of a 16 x 16 x 32 block from b0 of the side and k = 32 s on: lane l has side
   // b0 + l % 16, k = 32 s + 8 (l / 16) and the seven after it
   static __device__ __forceinline__ E8 frag(const char *lds, int p, int b0, int s) {
-    const int t = lane_id() & 15, g = lane_id() >> 4;
+    const int t = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4;
     lds += p * PLANE;
     if constexpr (KC) {
       return *reinterpret_cast<const E8 *>(lds + slot(b0 + t, 4 * s + g) * 16);
@@ -268,23 +253,102 @@ struct Operand {
 // number: the parts of an infinity (or of a float above the largest bf16) make
 // NaN of what is an infinity or a number
 template <bool IK, bool JK, bool HELD>
-__device__ __noinline__ float plain_chain(const GemmArgs &a, int64_t i, int j, int64_t k0,
-                                          int64_t k1) {
+__device__ float plain_chain(const LayerMat &A, const LayerMat &B, int64_t i, int j, int64_t k0,
+                             int64_t k1) {
   float s = 0.0f;
+#pragma unroll 1
   for (int64_t k = k0; k < k1; ++k) {
-    const float x = ((const float *)a.A.p)[IK ? i * a.A.ld + k : k * a.A.ld + i];
+    const float x = ((const float *)A.p)[IK ? i * A.ld + k : k * A.ld + i];
     float w;
     if constexpr (HELD) {
       float v[4];
-      const uint8_t b = ((const uint8_t *)a.B.p)[k * a.B.ld + j];
-      hold_unpack4(b, hold_scale(a.B.scale[k * (a.B.ld / 32) + j / 32]), a.B.hold, v);
+      const uint8_t b = ((const uint8_t *)B.p)[k * B.ld + j];
+      hold_unpack4(b, hold_scale(B.scale[k * (B.ld / 32) + j / 32]), B.hold, v);
       w = v[0];
     } else {
-      w = ((const float *)a.B.p)[JK ? j * a.B.ld + k : k * a.B.ld + j];
+      w = ((const float *)B.p)[JK ? j * B.ld + k : k * B.ld + j];
     }
     s = fmaf(x, w, s);
   }
   return s;
+}
+
+// A wave's outputs, rows i0.. and columns j0.., or their parts' sums, by way of LDS:
+// there a lane has four columns of a row in each block, and eight neighbouring
+// ones for the epilogue, so that a row's outputs are written whole.  lds: BYTES
+// of the wave's own; the chunks of four floats are exchanged by the row's number
+// against bank conflicts
+template <class T, int NI, int NJ, int BYTES, bool IK, bool JK, bool HELD, bool LIN>
+__device__ __forceinline__ void write_tile(const GemmArgs &a, const v4f (&acc)[NI][NJ], char *lds,
+                                           int64_t i0, int64_t j0, int64_t k0, int64_t k1) {
+  constexpr int W = 16 * NJ, CH = W / 4, LPR = W / 8;    // columns, chunks and lanes of a row
+  constexpr int FIT = BYTES / (16 * W * 4);              // blocks of rows that fit
+  constexpr int NB = FIT >= NI ? NI : FIT >= 4 ? 4 : FIT >= 2 ? 2 : 1;
+  static_assert(FIT >= 1 && NI % NB == 0, "whole passes");
+  const int lane = lane_id();
+  float4 *buf = reinterpret_cast<float4 *>(lds);
+#pragma unroll
+  for (int p = 0; p < NI; p += NB) {
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        const int row = 16 * i + (lane & 15), c = 4 * j + (lane >> 4);
+        const v4f v = acc[p + i][j];
+        buf[row * CH + (c ^ (row & 7))] = make_float4(v[0], v[1], v[2], v[3]);
+      }
+    // a wave's LDS accesses are carried out in order
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+    for (int s = 0; s < NB * 16 * LPR / WAVE; ++s) {
+      const int row = s * (WAVE / LPR) + lane / LPR, c = 2 * (lane % LPR);
+      const float4 x = buf[row * CH + (c ^ (row & 7))], y = buf[row * CH + ((c + 1) ^ (row & 7))];
+      float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+      const int64_t i = i0 + 16 * p + row, j = j0 + 4 * c;
+      if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+          if (!(fabsf(v[r]) < INFINITY) && i < a.I && j + r < a.J)
+            v[r] = plain_chain<IK, JK, HELD>(a.A, a.B, i, (int)j + r, k0, k1);
+      }
+      if (a.part) {
+        if (i < a.I && j < a.ldp) {
+          float4 *o = reinterpret_cast<float4 *>(a.part + ((int64_t)blockIdx.y * a.I + i) * a.ldp + j);
+          o[0] = make_float4(v[0], v[1], v[2], v[3]);
+          o[1] = make_float4(v[4], v[5], v[6], v[7]);
+        }
+      } else {
+        finish<T, LIN>(a, i, (int)j, i < a.I, v);
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// The products of a K-tile in LDS
+template <class OA, class OB, int NI, int NJ>
+__device__ __forceinline__ void multiply(const char *la, const char *lb, int wi, int wj,
+                                         v4f (&acc)[NI][NJ]) {
+  constexpr int P = OA::P;
+#pragma unroll
+  for (int s = 0; s < OA::BK / 32; ++s) {
+    typename OA::E8 fi[P][NI], fj[P][NJ];
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+#pragma unroll
+      for (int i = 0; i < NI; ++i) fi[p][i] = OA::frag(la, p, wi + 16 * i, s);
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) fj[p][j] = OB::frag(lb, p, wj + 16 * j, s);
+    }
+#pragma unroll
+    for (int q = P - 1; q >= 0; --q)       // the small products first
+#pragma unroll
+      for (int p = 0; p <= q; ++p)
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) acc[i][j] = mma(fj[q - p][j], fi[p][i], acc[i][j]);
+  }
 }
 
 // A block of 256 threads owns a TI x TJ tile, each wave a quarter of it in
@@ -292,11 +356,10 @@ __device__ __noinline__ float plain_chain(const GemmArgs &a, int64_t i, int j, i
 // multiplied.  Blocks go to the eight XCDs in turn: each XCD takes a run of
 // neighbouring tiles, so that their operands meet in its L2.
 template <class T, int TI, int TJ, bool IK, bool JK, bool HELD, bool LIN>
-__global__ void __launch_bounds__(256) k_gemm(GemmArgs a) {
+__global__ void __launch_bounds__(256, 2) k_gemm(GemmArgs a) {
   typedef Operand<T, TI, IK, false> OA;
   typedef Operand<T, TJ, JK, HELD> OB;
-  typedef typename OA::E8 E8;
-  constexpr int BK = OA::BK, P = OA::P, NBUF = Tile<T>::NBUF;
+  constexpr int BK = OA::BK, NBUF = Tile<T>::NBUF;
   constexpr int NI = TI / 32, NJ = TJ / 32;
   __shared__ __attribute__((aligned(16))) char lds[NBUF][OA::BYTES + OB::BYTES];
   const int lane = lane_id(), wave = threadIdx.x / WAVE;
@@ -340,26 +403,7 @@ __global__ void __launch_bounds__(256) k_gemm(GemmArgs a) {
     for (int64_t k = k0; k < k1; k += BK) {
       const bool more = k + BK < k1;
       if (more) fetch(k + BK);
-#pragma unroll
-      for (int s = 0; s < BK / 32; ++s) {
-        E8 fi[P][NI], fj[P][NJ];
-#pragma unroll
-        for (int p = 0; p < P; ++p) {
-#pragma unroll
-          for (int i = 0; i < NI; ++i) fi[p][i] = OA::frag(lds[buf], p, wi + 16 * i, s);
-#pragma unroll
-          for (int j = 0; j < NJ; ++j)
-            fj[p][j] = OB::frag(lds[buf] + OA::BYTES, p, wj + 16 * j, s);
-        }
-#pragma unroll
-        for (int q = P - 1; q >= 0; --q)       // the small products first
-#pragma unroll
-          for (int p = 0; p <= q; ++p)
-#pragma unroll
-            for (int i = 0; i < NI; ++i)
-#pragma unroll
-              for (int j = 0; j < NJ; ++j) acc[i][j] = mma(fj[q - p][j], fi[p][i], acc[i][j]);
-      }
+      multiply<OA, OB>(lds[buf], lds[buf] + OA::BYTES, wi, wj, acc);
       if (NBUF == 1) __syncthreads();
       if (more) {
         if (NBUF == 2) buf ^= 1;
@@ -367,66 +411,97 @@ __global__ void __launch_bounds__(256) k_gemm(GemmArgs a) {
         __syncthreads();
       }
     }
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int64_t row = i0 + wi + 16 * i + (lane & 15);
-#pragma unroll
-      for (int j2 = 0; j2 < NJ; j2 += 2) {
-        const int64_t c0 = j0 + wj + 16 * j2;
-        if (c0 >= a.J) continue;   // the whole wave together
-        float v[2][4];
-#pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            v[b][r] = acc[i][j2 + b][r];
-            if constexpr (P == 3) {
-              const int64_t c = c0 + 16 * b + 4 * (lane >> 4) + r;
-              if (!(fabsf(v[b][r]) < INFINITY) && row < a.I && c < a.J)
-                v[b][r] = plain_chain<IK, JK, HELD>(a, row, (int)c, k0, k1);
-            }
-          }
-        if (a.part) {
-          float *o = a.part + ((int64_t)blockIdx.y * a.I + row) * a.ldp + c0 + 4 * (lane >> 4);
-#pragma unroll
-          for (int b = 0; b < 2; ++b)
-            if (row < a.I)
-              *reinterpret_cast<float4 *>(o + 16 * b) =
-                  make_float4(v[b][0], v[b][1], v[b][2], v[b][3]);
-        } else {
-          finish<T, LIN>(a, row, (int)c0, row < a.I, v);
-        }
-      }
-    }
+    __syncthreads();   // the last K-tile has been read
+    constexpr int MINE = sizeof lds / 4;
+    write_tile<T, NI, NJ, MINE, IK, JK, HELD, LIN>(a, acc, (char *)lds + wave * MINE, i0 + wi,
+                                                   j0 + wj, k0, k1);
   }
 }
 
-// The parts' sums, in order, and the epilogue: a wave per 16 rows x 32 columns
+// The same for 16-bit operands whose rows lie on 16-byte boundaries: K-tiles go
+// straight from memory into LDS, the next one while this one is multiplied.
+// WI x WJ waves; each reads (TI / WI + TJ / WJ) x 128 bytes of LDS per K-tile for
+// TI / WI x TJ / WJ outputs
+template <class T, int TI, int TJ, int WI, int WJ, bool IK, bool JK, bool LIN>
+__global__ void __launch_bounds__(WI *WJ *WAVE, 2) k_gemm_dma(GemmArgs a) {
+  constexpr int NT = WI * WJ * WAVE, NI = TI / WI / 16, NJ = TJ / WJ / 16;
+  typedef Operand<T, TI, IK, false, NT> OA;
+  typedef Operand<T, TJ, JK, false, NT> OB;
+  constexpr int BK = OA::BK, BUF = OA::BYTES + OB::BYTES;
+  __shared__ __attribute__((aligned(16))) char lds[2 * BUF];
+  const int wave = threadIdx.x / WAVE;
+  const int wi = TI / WI * (wave % WI), wj = TJ / WJ * (wave / WI);
+  const int64_t tj = (a.J + TJ - 1) / TJ, tiles = (a.I + TI - 1) / TI * tj;
+  const int64_t per = (tiles + 7) / 8;
+  const int64_t k0 = (int64_t)blockIdx.y * a.kchunk;
+  const int64_t k1 = k0 + a.kchunk < a.K ? k0 + a.kchunk : a.K;
+  for (int64_t u = blockIdx.x; u < 8 * per; u += gridDim.x) {
+    const int64_t t = (u & 7) * per + (u >> 3);
+    if (t >= tiles) continue;   // the whole block together
+    const int64_t i0 = t / tj * TI, j0 = t % tj * TJ;
+    uint32_t oa[OA::N], ob[OB::N];
+    OA::dma_offsets(a.A, i0, a.I, oa);
+    OB::dma_offsets(a.B, j0, a.J, ob);
+    const T *pa = (const T *)a.A.p + (IK ? i0 * a.A.ld + k0 : k0 * a.A.ld + i0);
+    const T *pb = (const T *)a.B.p + (JK ? j0 * a.B.ld + k0 : k0 * a.B.ld + j0);
+    const int64_t sa = IK ? BK : BK * a.A.ld, sb = JK ? BK : BK * a.B.ld;
+    auto fetch = [&](int64_t k, int buf) {
+      char *da = lds + buf * BUF, *db = da + OA::BYTES;
+      if (k + BK <= k1) {
+        OA::template dma<true>(pa, oa, da, BK);
+        OB::template dma<true>(pb, ob, db, BK);
+      } else {   // the last, short one
+        OA::template dma<false>(pa, oa, da, (int)(k1 - k));
+        OB::template dma<false>(pb, ob, db, (int)(k1 - k));
+      }
+      pa += sa;
+      pb += sb;
+    };
+    v4f acc[NI][NJ];
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
+    __syncthreads();   // the tile before has been read
+    if (k0 < k1) fetch(k0, 0);
+    int buf = 0;
+    for (int64_t k = k0; k < k1; k += BK, buf ^= 1) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      if (k + BK < k1) fetch(k + BK, buf ^ 1);
+      multiply<OA, OB>(lds + buf * BUF, lds + buf * BUF + OA::BYTES, wi, wj, acc);
+    }
+    __syncthreads();   // the last K-tile has been read
+    constexpr int MINE = sizeof lds / (WI * WJ);
+    write_tile<T, NI, NJ, MINE, IK, JK, false, LIN>(a, acc, lds + wave * MINE, i0 + wi, j0 + wj,
+                                                    k0, k1);
+  }
+}
+
+// The parts' sums, in order, and the epilogue: eight columns of a row per thread
 template <class T, bool LIN>
 __global__ void __launch_bounds__(256) k_gemm_join(GemmArgs a, int parts) {
-  const int lane = threadIdx.x & 63;
-  const int64_t gj = (a.J + 31) / 32, units = (a.I + 15) / 16 * gj;
-  for (int64_t u = (int64_t)blockIdx.x * 4 + threadIdx.x / WAVE; u < units;
-       u += (int64_t)gridDim.x * 4) {
-    const int64_t row = u / gj * 16 + (lane & 15);
-    const int j0 = (int)(u % gj) * 32;
-    const int64_t at = (row < a.I ? row : a.I - 1) * a.ldp + j0 + 4 * (lane >> 4);
-    float v[2][4] = {};
-    for (int s = 0; s < parts; ++s)
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const float4 p = *reinterpret_cast<const float4 *>(a.part + (int64_t)s * a.I * a.ldp + at +
-                                                           16 * b);
-        v[b][0] += p.x, v[b][1] += p.y, v[b][2] += p.z, v[b][3] += p.w;
-      }
-    finish<T, LIN>(a, row, j0, row < a.I, v);
+  const int64_t per = a.ldp / 8, units = a.I * per;   // whole quads per row
+  for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < units;
+       u += (int64_t)gridDim.x * 256) {
+    const int64_t i = u / per;
+    const int j = (int)(u - i * per) * 8;
+    float v[8] = {};
+    for (int s = 0; s < parts; ++s) {
+      const float4 *p =
+          reinterpret_cast<const float4 *>(a.part + ((int64_t)s * a.I + i) * a.ldp + j);
+      const float4 x = p[0], y = p[1];
+      v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
+      v[4] += y.x, v[5] += y.y, v[6] += y.z, v[7] += y.w;
+    }
+    finish<T, LIN>(a, i, j, true, v);
   }
 }
 
 // dz = dy act'(pre) of `rows` rows per block, rounded to the type (dz NULL: not
 // wanted), and its column sums over them (part NULL: not wanted).  The 256
 // threads are 256 / ct rows of ct threads, eight columns each
-template <class T, bool VEC>
+template <class T>
 __global__ void __launch_bounds__(256) k_act_grad(LinearGradArgs a, int64_t rows, int ct, T *dz,
                                                   int64_t ldz, float *part) {
   __shared__ float red[256][9];
@@ -438,17 +513,17 @@ __global__ void __launch_bounds__(256) k_act_grad(LinearGradArgs a, int64_t rows
   if (c0 < a.n)
     for (int64_t r = r0 + tr; r < r1; r += rt) {
       float v[8], z[8];
-      load8<T, VEC>((const T *)a.dy + r * a.lddy, c0, a.n, v);
+      load8((const T *)a.dy + r * a.lddy, c0, a.n, v);
       if (a.act != NR_ACT_NONE) {
         if (a.pre.hold)
           read8<T>((const uint8_t *)a.pre.p + r * a.pre.ld, a.pre.scale + r * (a.pre.ld / 32), c0,
                 a.pre.hold, z);
         else
-          load8<T, VEC>((const T *)a.pre.p + r * a.pre.ld, c0, a.n, z);
+          load8((const T *)a.pre.p + r * a.pre.ld, c0, a.n, z);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] *= act_slope<exact>(z[i], a.act);
       }
-      if (dz) store8<T, true>(dz + r * ldz, c0, a.n, v);
+      if (dz) store8(dz + r * ldz, c0, a.n, v);
 #pragma unroll
       for (int i = 0; i < 8; ++i) s[i] += c0 + i < a.n ? v[i] : 0.0f;
     }
@@ -473,16 +548,17 @@ static bool aligned(const void *p, int64_t ld, size_t e, size_t to) {
   return !p || (reinterpret_cast<uintptr_t>(p) % to == 0 && ld * e % to == 0);
 }
 
-// How a product is cut: the tile's side, and parts of k.  128 x 128 tiles read
-// half of what 64 x 64 ones do, if there are enough of them to go round
+// How a product is cut: the tile's side, and parts of k.  Larger tiles read less
+// of LDS and memory for an output, if there are enough of them to go round
 struct Split {
   int side, parts;
   int64_t kchunk;
 };
-static Split split_of(int64_t I, int J, int64_t K) {
+static Split split_of(int64_t I, int J, int64_t K, int dtype) {
   auto tiles = [&](int64_t t) { return up(I, t) / t * (up(J, t) / t); };
   Split sp{128, 1, 64};
-  if (tiles(128) < 256 && tiles(128) * (K / 512) < 256) sp.side = 64;
+  if (dtype != NR_F32 && tiles(256) >= 256) sp.side = 256;
+  else if (tiles(128) < 256 && tiles(128) * (K / 512) < 256) sp.side = 64;
   const int64_t n = tiles(sp.side);
   int64_t parts = n > 0 && n < 256 ? (512 + n - 1) / n : 1;
   const int64_t most = K / 256 < 64 ? K / 256 : 64;
@@ -492,42 +568,67 @@ static Split split_of(int64_t I, int J, int64_t K) {
   sp.parts = K > 0 ? (int)((K + sp.kchunk - 1) / sp.kchunk) : 1;
   return sp;
 }
-static size_t part_bytes(int64_t I, int J, int64_t K) {
-  const Split sp = split_of(I, J, K);
+static size_t part_bytes(int64_t I, int J, int64_t K, int dtype) {
+  const Split sp = split_of(I, J, K, dtype);
   return sp.parts > 1 ? sizeof(float) * (size_t)sp.parts * I * up(J, 32) : 0;
+}
+
+template <class T>
+static constexpr int type_of() {
+  return sizeof(T) == 4 ? NR_F32 : __is_same(T, bf16_t) ? NR_BF16 : NR_F16;
+}
+
+// an operand that can go straight into LDS: whole chunks in rows on 16-byte
+// boundaries, a tile of them within 2^32 bytes
+static bool direct(const LayerMat &m, int64_t width) {
+  return !m.hold && aligned(m.p, m.ld, 2, 16) && m.ld < (int64_t)1 << 22 && width % 8 == 0;
 }
 
 template <class T, int S, bool IK, bool JK, bool LIN>
 static void gemm_tiles(const GemmArgs &a, int parts, hipStream_t s) {
   const int64_t tiles = up(up(a.I, S) / S * (up(a.J, S) / S), 8);
   const dim3 g((unsigned)(tiles < 1 << 22 ? tiles : 1 << 22), parts);
-  if constexpr (!IK) {
-    if (a.B.hold) {
-      hipLaunchKernelGGL((k_gemm<T, S, S, IK, JK, true, LIN>), g, dim3(256), 0, s, a);
+  if constexpr (sizeof(T) == 2 && S >= 128) {
+    if (direct(a.A, IK ? a.K : a.I) && direct(a.B, JK ? a.K : a.J)) {
+      if constexpr (S == 256)
+        hipLaunchKernelGGL((k_gemm_dma<T, S, S, 2, 4, IK, JK, LIN>), g, dim3(512), 0, s, a);
+      else
+        hipLaunchKernelGGL((k_gemm_dma<T, S, S, 2, 2, IK, JK, LIN>), g, dim3(256), 0, s, a);
       return;
     }
   }
-  hipLaunchKernelGGL((k_gemm<T, S, S, IK, JK, false, LIN>), g, dim3(256), 0, s, a);
+  if constexpr (S < 256) {
+    if constexpr (!IK) {
+      if (a.B.hold) {
+        hipLaunchKernelGGL((k_gemm<T, S, S, IK, JK, true, LIN>), g, dim3(256), 0, s, a);
+        return;
+      }
+    }
+    hipLaunchKernelGGL((k_gemm<T, S, S, IK, JK, false, LIN>), g, dim3(256), 0, s, a);
+  } else {
+    gemm_tiles<T, 128, IK, JK, LIN>(a, parts, s);
+  }
 }
 
 template <class T, bool IK, bool JK, bool LIN>
 static hipError_t gemm(GemmArgs a, float *ws, hipStream_t s) {
   if (a.I <= 0) return hipSuccess;
-  const Split sp = split_of(a.I, a.J, a.K);
+  const Split sp = split_of(a.I, a.J, a.K, type_of<T>());
   a.kchunk = sp.kchunk;
   a.part = sp.parts > 1 ? ws : nullptr;
   a.ldp = up(a.J, 32);
-  if (sp.side == 128) gemm_tiles<T, 128, IK, JK, LIN>(a, sp.parts, s);
-  else gemm_tiles<T, 64, IK, JK, LIN>(a, sp.parts, s);
+  if (sp.side == 64) gemm_tiles<T, 64, IK, JK, LIN>(a, sp.parts, s);
+  else if (sizeof(T) == 4 || sp.side == 128) gemm_tiles<T, 128, IK, JK, LIN>(a, sp.parts, s);
+  else if constexpr (sizeof(T) == 2) gemm_tiles<T, 256, IK, JK, LIN>(a, sp.parts, s);
   if (sp.parts > 1) {
-    const int64_t blocks = (up(a.I, 16) / 16 * (up(a.J, 32) / 32) + 3) / 4;
+    const int64_t blocks = (a.I * (a.ldp / 8) + 255) / 256;
     hipLaunchKernelGGL((k_gemm_join<T, LIN>), dim3((unsigned)(blocks < 1 << 20 ? blocks : 1 << 20)),
                        dim3(256), 0, s, a, sp.parts);
   }
   return hipGetLastError();
 }
 
-size_t linear_ws(int64_t m, int n, int k, int dtype) { return part_bytes(m, n, k); }
+size_t linear_ws(int64_t m, int n, int k, int dtype) { return part_bytes(m, n, k, dtype); }
 
 template <class T>
 static hipError_t linear_t(const LinearArgs &l, void *ws, hipStream_t s) {
@@ -535,9 +636,6 @@ static hipError_t linear_t(const LinearArgs &l, void *ws, hipStream_t s) {
   a.I = l.m, a.J = l.n, a.K = l.k;
   a.A = LayerMat{l.x, l.ldx, 0, nullptr};
   a.B = LayerMat{l.w, l.ldw, 0, nullptr};
-  a.vec = aligned(l.y, l.ldy, sizeof(T), 4 * sizeof(T)) &&
-          aligned(l.res, l.ldr, sizeof(T), 4 * sizeof(T)) &&
-          (l.pre_hold || aligned(l.pre, l.ldp, sizeof(T), 4 * sizeof(T)));
   a.lin = l;
   return gemm<T, true, true, true>(a, (float *)ws, s);
 }
@@ -572,7 +670,8 @@ static GradPlan grad_plan(const LinearGradArgs &a, int dtype) {
   p.at_part = off;
   if (a.db) off += up(sizeof(float) * (size_t)p.nb * a.n, 256);
   p.at_prod = off;
-  const size_t px = a.dx ? part_bytes(a.m, a.k, a.n) : 0, pw = a.dw ? part_bytes(a.n, a.k, a.m) : 0;
+  const size_t px = a.dx ? part_bytes(a.m, a.k, a.n, dtype) : 0;
+  const size_t pw = a.dw ? part_bytes(a.n, a.k, a.m, dtype) : 0;
   p.bytes = off + (px > pw ? px : pw);
   return p;
 }
@@ -586,12 +685,8 @@ static hipError_t linear_grad_t(const LinearGradArgs &l, int dtype, char *ws, hi
   float *part = l.db ? (float *)(ws + p.at_part) : nullptr;
   float *prod = (float *)(ws + p.at_prod);
   if (p.act && l.m > 0) {
-    const bool vec = aligned(l.dy, l.lddy, sizeof(T), 16) &&
-                     (l.act == NR_ACT_NONE || l.pre.hold ||
-                      aligned(l.pre.p, l.pre.ld, sizeof(T), 16));
     const dim3 g((unsigned)p.nb, (l.n + 8 * p.ct - 1) / (8 * p.ct));
-    hipLaunchKernelGGL((vec ? k_act_grad<T, true> : k_act_grad<T, false>), g, dim3(256), 0, s, l,
-                       p.rows, p.ct, dz, p.ldz, part);
+    hipLaunchKernelGGL(k_act_grad<T>, g, dim3(256), 0, s, l, p.rows, p.ct, dz, p.ldz, part);
   }
   hipError_t e = hipGetLastError();
   if (l.db && e == hipSuccess) e = launch_col_join(part, p.nb, l.n, l.n, dtype, l.db, s);
@@ -602,7 +697,6 @@ static hipError_t linear_grad_t(const LinearGradArgs &l, int dtype, char *ws, hi
     a.A = z;
     a.B = LayerMat{l.w, l.ldw, 0, nullptr};
     a.out = l.dx, a.ldo = l.lddx;
-    a.vec = aligned(l.dx, l.lddx, sizeof(T), 4 * sizeof(T));
     e = gemm<T, true, false, false>(a, prod, s);
   }
   if (l.dw && e == hipSuccess) {
@@ -611,7 +705,6 @@ static hipError_t linear_grad_t(const LinearGradArgs &l, int dtype, char *ws, hi
     a.A = z;
     a.B = l.x;
     a.out = l.dw, a.ldo = l.lddw;
-    a.vec = aligned(l.dw, l.lddw, sizeof(T), 4 * sizeof(T));
     e = gemm<T, false, false, false>(a, prod, s);
   }
   return e;

@@ -24,15 +24,15 @@ __device__ __forceinline__ void block_sum(float (&v)[N], float (*red)[4]) {
 }
 
 // eight elements of a row of the type, or of one held in 8 bits
-template <class T, bool VEC>
+template <class T>
 __device__ __forceinline__ void row8(const LayerMat &a, int64_t r, int c0, int d, float (&v)[8]) {
   if (a.hold)
     read8<T>((const uint8_t *)a.p + r * a.ld, a.scale + r * (a.ld / 32), c0, a.hold, v);
   else
-    load8<T, VEC>((const T *)a.p + r * a.ld, c0, d, v);
+    load8((const T *)a.p + r * a.ld, c0, d, v);
 }
 
-template <class T, bool VEC>
+template <class T>
 __global__ void __launch_bounds__(256) k_norm(NormArgs a) {
   __shared__ float red[1][4];
   constexpr bool half = __is_same(T, f16_t);
@@ -41,7 +41,7 @@ __global__ void __launch_bounds__(256) k_norm(NormArgs a) {
     const T *x = (const T *)a.x + r * a.ldx;
     float v[8], s[1] = {0.0f};
     for (int c = threadIdx.x * 8; c < d; c += 2048) {
-      load8<T, VEC>(x, c, d, v);
+      load8(x, c, d, v);
 #pragma unroll
       for (int i = 0; i < 8; ++i) s[0] += v[i];
     }
@@ -49,7 +49,7 @@ __global__ void __launch_bounds__(256) k_norm(NormArgs a) {
     const float mu = s[0] / (float)d;
     s[0] = 0.0f;
     for (int c = threadIdx.x * 8; c < d; c += 2048) {
-      load8<T, VEC>(x, c, d, v);
+      load8(x, c, d, v);
 #pragma unroll
       for (int i = 0; i < 8; ++i) s[0] += c + i < d ? (v[i] - mu) * (v[i] - mu) : 0.0f;
     }
@@ -61,22 +61,22 @@ __global__ void __launch_bounds__(256) k_norm(NormArgs a) {
     }
     for (int c = threadIdx.x * 8; c < dp; c += 2048) {
       float g[8], b[8];
-      load8<T, VEC>(x, c, d, v);
+      load8(x, c, d, v);
       if (a.x_hold) write8(a.xq + r * dp, a.xs + r * (dp / 32), c, a.x_hold, half, v);
-      if (a.g) load8<T, false>((const T *)a.g, c, d, g);
-      if (a.b) load8<T, false>((const T *)a.b, c, d, b);
+      if (a.g) load8((const T *)a.g, c, d, g);
+      if (a.b) load8((const T *)a.b, c, d, b);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         v[i] = (v[i] - mu) * rs * (a.g ? g[i] : 1.0f) + (a.b ? b[i] : 0.0f);
         v[i] = c + i < d ? to_f32(from_f32<T>(v[i])) : 0.0f;
       }
-      store8<T, VEC>((T *)a.y + r * a.ldy, c, d, v);
+      store8((T *)a.y + r * a.ldy, c, d, v);
       if (a.y_hold) write8(a.yq + r * dp, a.ys + r * (dp / 32), c, a.y_hold, half, v);
     }
   }
 }
 
-template <class T, bool VEC>
+template <class T>
 __global__ void __launch_bounds__(256) k_norm_dx(NormGradArgs a) {
   __shared__ float red[2][4];
   const int d = a.d;
@@ -85,9 +85,9 @@ __global__ void __launch_bounds__(256) k_norm_dx(NormGradArgs a) {
     const float mu = a.mean[r], rs = a.rstd[r];
     float x[8], u[8], g[8], s[2] = {0.0f, 0.0f};
     for (int c = threadIdx.x * 8; c < d; c += 2048) {
-      row8<T, VEC>(a.x, r, c, d, x);
-      load8<T, VEC>(dy, c, d, u);
-      if (a.g) load8<T, false>((const T *)a.g, c, d, g);
+      row8<T>(a.x, r, c, d, x);
+      load8(dy, c, d, u);
+      if (a.g) load8((const T *)a.g, c, d, g);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         if (c + i >= d) continue;
@@ -99,18 +99,18 @@ __global__ void __launch_bounds__(256) k_norm_dx(NormGradArgs a) {
     block_sum(s, red);
     const float m1 = s[0] / (float)d, m2 = s[1] / (float)d;
     for (int c = threadIdx.x * 8; c < d; c += 2048) {
-      row8<T, VEC>(a.x, r, c, d, x);
-      load8<T, VEC>(dy, c, d, u);
-      if (a.g) load8<T, false>((const T *)a.g, c, d, g);
+      row8<T>(a.x, r, c, d, x);
+      load8(dy, c, d, u);
+      if (a.g) load8((const T *)a.g, c, d, g);
 #pragma unroll
       for (int i = 0; i < 8; ++i)
         u[i] = rs * ((a.g ? u[i] * g[i] : u[i]) - m1 - (x[i] - mu) * rs * m2);
       if (a.add) {
-        load8<T, VEC>((const T *)a.add + r * a.ldadd, c, d, x);
+        load8((const T *)a.add + r * a.ldadd, c, d, x);
 #pragma unroll
         for (int i = 0; i < 8; ++i) u[i] += x[i];
       }
-      store8<T, VEC>((T *)a.dx + r * a.lddx, c, d, u);
+      store8((T *)a.dx + r * a.lddx, c, d, u);
     }
   }
 }
@@ -126,8 +126,8 @@ __global__ void __launch_bounds__(256) k_norm_cols(NormGradArgs a, int64_t rows,
   for (int64_t r = r0; r < r1; ++r) {
     const float mu = a.mean[r], rs = a.rstd[r];
     float x[8], u[8];
-    row8<T, false>(a.x, r, c0, a.d, x);
-    load8<T, false>((const T *)a.dy + r * a.lddy, c0, a.d, u);
+    row8<T>(a.x, r, c0, a.d, x);
+    load8((const T *)a.dy + r * a.lddy, c0, a.d, u);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       sg[i] += u[i] * ((x[i] - mu) * rs);
@@ -174,15 +174,11 @@ hipError_t launch_col_join(const float *partial, int64_t rows, int64_t ld, int d
   return hipGetLastError();
 }
 
-static bool aligned16(const void *p, int64_t ld, size_t e) {
-  return !p || (reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * e % 16 == 0);
-}
 static unsigned row_grid(int64_t m) { return (unsigned)(m < 1 << 20 ? m : 1 << 20); }
 
 template <class T>
 static hipError_t norm_t(const NormArgs &a, hipStream_t s) {
-  const bool vec = aligned16(a.x, a.ldx, sizeof(T)) && aligned16(a.y, a.ldy, sizeof(T));
-  hipLaunchKernelGGL((vec ? k_norm<T, true> : k_norm<T, false>), dim3(row_grid(a.m)), dim3(256), 0,
+  hipLaunchKernelGGL(k_norm<T>, dim3(row_grid(a.m)), dim3(256), 0,
                      s, a);
   return hipGetLastError();
 }
@@ -208,13 +204,8 @@ size_t norm_grad_ws(const NormGradArgs &a) {
 
 template <class T>
 static hipError_t norm_grad_t(const NormGradArgs &a, int dtype, float *ws, hipStream_t s) {
-  const size_t e = sizeof(T);
-  if (a.dx && a.m > 0) {
-    const bool vec = aligned16(a.dy, a.lddy, e) && (a.x.hold || aligned16(a.x.p, a.x.ld, e)) &&
-                     aligned16(a.add, a.ldadd, e) && aligned16(a.dx, a.lddx, e);
-    hipLaunchKernelGGL((vec ? k_norm_dx<T, true> : k_norm_dx<T, false>), dim3(row_grid(a.m)),
-                       dim3(256), 0, s, a);
-  }
+  if (a.dx && a.m > 0)
+    hipLaunchKernelGGL(k_norm_dx<T>, dim3(row_grid(a.m)), dim3(256), 0, s, a);
   if (a.dg || a.db) {
     const int64_t rows = col_rows(a.m), nb = (a.m + rows - 1) / rows;
     float *pg = ws, *pb = ws + nb * a.d;

@@ -107,41 +107,31 @@ __device__ __forceinline__ float to_f32(T v) { return (float)v; }
 template <class T>
 __device__ __forceinline__ T from_f32(float v) { return (T)v; }   // to nearest, ties to even
 
-// eight elements of a row from column c0 on, zero past d.  VEC: the row starts
-// on a 16-byte boundary and c0 is a multiple of 8
-template <class T, bool VEC>
+// eight elements of a row from column c0 on, zero past d: one 16-byte access (two
+// for fp32) wherever the row starts, which costs nothing on a 16-byte boundary
+// and little off it
+template <class T>
 __device__ __forceinline__ void load8(const T *row, int c0, int d, float (&v)[8]) {
-  if (VEC && c0 + 8 <= d) {
-    if constexpr (sizeof(T) == 4) {
-      const float4 a = *reinterpret_cast<const float4 *>(row + c0);
-      const float4 b = *reinterpret_cast<const float4 *>(row + c0 + 4);
-      v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
-      v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-    } else {
-      typedef T t8 __attribute__((ext_vector_type(8)));
-      const t8 a = *reinterpret_cast<const t8 *>(row + c0);
+  typedef T t8 __attribute__((ext_vector_type(8)));
+  if (c0 + 8 <= d) {
+    t8 a;
+    __builtin_memcpy(&a, row + c0, sizeof a);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = to_f32(a[i]);
-    }
+    for (int i = 0; i < 8; ++i) v[i] = to_f32(a[i]);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = c0 + i < d ? to_f32(row[c0 + i]) : 0.0f;
   }
 }
 
-template <class T, bool VEC>
+template <class T>
 __device__ __forceinline__ void store8(T *row, int c0, int d, const float (&v)[8]) {
-  if (VEC && c0 + 8 <= d) {
-    if constexpr (sizeof(T) == 4) {
-      *reinterpret_cast<float4 *>(row + c0) = make_float4(v[0], v[1], v[2], v[3]);
-      *reinterpret_cast<float4 *>(row + c0 + 4) = make_float4(v[4], v[5], v[6], v[7]);
-    } else {
-      typedef T t8 __attribute__((ext_vector_type(8)));
-      t8 a;
+  typedef T t8 __attribute__((ext_vector_type(8)));
+  if (c0 + 8 <= d) {
+    t8 a;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) a[i] = from_f32<T>(v[i]);
-      *reinterpret_cast<t8 *>(row + c0) = a;
-    }
+    for (int i = 0; i < 8; ++i) a[i] = from_f32<T>(v[i]);
+    __builtin_memcpy(row + c0, &a, sizeof a);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)

@@ -140,6 +140,29 @@ def test_linear_grad(m, k, n, t):
 
 
 @pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("m,k,n", [(4200, 200, 4104), (200, 4200, 4104), (4200, 4104, 200),
+                                   (4097, 72, 4099), (16_400, 1030, 264), (9000, 520, 48)])
+def test_linear_many_tiles(m, k, n, t):
+    # each product with more outputs than the chip takes at once, its ends inside tiles
+    g, dt, x, w, b, r = linear_case(m, k, n, t)
+    y, z = NR.nr_linear(x, w, b, act="gelu", residual=r, pre=True)
+    check_linear(x, w, b, r, "gelu", y, z)
+    dy = rows(g, m, n, dt, scale=0.1)
+    got = NR.nr_linear_grad(dy, x, w, act="gelu", pre=z)
+    grad_check(dy, x, w, "gelu", z, got, t != "f32")
+    for fmt in ("i8", "e4m3"):
+        h, hx = NR.nr_act_hold(z, fmt), NR.nr_act_hold(x, fmt)
+        y2, hz = NR.nr_linear(x, w, b, act="gelu", residual=r, pre=fmt)
+        assert torch.equal(y, y2) and torch.equal(h.scale, hz.scale)
+        assert torch.equal(h.q.view(torch.uint8), hz.q.view(torch.uint8))
+        got = NR.nr_linear_grad(dy, hx, w, act="gelu", pre=hz)
+        want = NR.nr_linear_grad(dy, NR.nr_act_read(hx), w, act="gelu", pre=NR.nr_act_read(hz))
+        # one held: another path for dw, the same products in the same order
+        grad_check(dy, NR.nr_act_read(hx), w, "gelu", NR.nr_act_read(hz), got, t != "f32")
+        assert torch.equal(got[0], want[0]) and torch.equal(got[2], want[2])
+
+
+@pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("pad", [1, 8, 13])
 def test_linear_grad_strides(pad, t):
     for m, k, n in ((70, 64, 96), (5, 200, 33), (200, 65, 66)):
