@@ -689,7 +689,7 @@ static hipError_t linear_grad_t(const LinearGradArgs &l, int dtype, char *ws, hi
     hipLaunchKernelGGL(k_act_grad<T>, g, dim3(256), 0, s, l, p.rows, p.ct, dz, p.ldz, part);
   }
   hipError_t e = hipGetLastError();
-  if (l.db && e == hipSuccess) e = launch_col_join(part, p.nb, l.n, l.n, dtype, l.db, s);
+  if (l.db && e == hipSuccess) e = launch_col_join(part, l.db, nullptr, nullptr, p.nb, l.n, dtype, s);
   const LayerMat z = p.dz ? LayerMat{dz, p.ldz, 0, nullptr} : LayerMat{l.dy, l.lddy, 0, nullptr};
   if (l.dx && e == hipSuccess) {
     GemmArgs a{};

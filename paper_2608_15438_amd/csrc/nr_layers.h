@@ -95,10 +95,11 @@ hipError_t launch_hold(const void *x, int64_t ldx, int64_t m, int d, int dtype, 
                        uint8_t *q, uint8_t *scale, hipStream_t s);
 hipError_t launch_read(const uint8_t *q, const uint8_t *scale, int64_t m, int d, int hold,
                        int dtype, void *y, int64_t ldy, hipStream_t s);
-// out[c] = sum over r of partial[r][c] (rows of ld floats), rounded to the type;
-// the rows are added in a fixed order
-hipError_t launch_col_join(const float *partial, int64_t rows, int64_t ld, int d, int dtype,
-                           void *out, hipStream_t s);
+// out[c] = sum over r of partial[r][c] (rows of d floats), rounded to the type; the
+// rows are added in a fixed order.  Two such sums in one launch; out NULL: not
+// wanted
+hipError_t launch_col_join(const float *p0, void *out0, const float *p1, void *out1, int64_t rows,
+                           int d, int dtype, hipStream_t s);
 
 // ---------------------------------------------------------------- elements
 
@@ -138,6 +139,22 @@ __device__ __forceinline__ void store8(T *row, int c0, int d, const float (&v)[8
       if (c0 + i < d) row[c0 + i] = from_f32<T>(v[i]);
   }
 }
+
+// eight elements as they are in memory
+template <class T>
+struct Raw8 {
+  typedef T t8 __attribute__((ext_vector_type(8)));
+  t8 v;
+  __device__ __forceinline__ void load(const T *row, int c0, int d) {
+    if (c0 + 8 <= d) {
+      __builtin_memcpy(&v, row + c0, sizeof v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = c0 + i < d ? row[c0 + i] : (T)0.0f;
+    }
+  }
+  __device__ __forceinline__ float operator[](int i) const { return to_f32(v[i]); }
+};
 
 // ---------------------------------------------------------------- 8 bits
 
