@@ -9,6 +9,8 @@
 // neighbouring elements of a row of the output.  Where the tiles are few and k
 // long, k is cut and the parts' fp32 sums are added in order by a second kernel
 // with the same epilogue.
+#include <type_traits>
+
 #include "nr_layers.h"
 
 namespace nr {
@@ -213,21 +215,24 @@ struct Operand {
       offset[u] = (uint32_t)(row * m.ld + 8 * c) * (uint32_t)sizeof(T);
     }
   }
-  // k of the chunks within the tile from `left` on: zeros
+  // (in asm, so that the compiler does not wait for them before every read of LDS;
+  // arrived() does, once a K-tile).  k of the chunks from `left` on: zeros
   template <bool FULL>
-  static __device__ __forceinline__ void dma(const T *base, const uint32_t (&offset)[N], char *lds,
-                                             int left) {
-    typedef __attribute__((address_space(1))) const char *global_t;
-    typedef __attribute__((address_space(3))) char *lds_t;
-    lds += threadIdx.x / WAVE * 1024;
+  static __device__ __forceinline__ void dma(const T *base, const uint32_t (&offset)[N],
+                                             uint32_t lds, int left) {
+    const uint32_t at = __builtin_amdgcn_readfirstlane(lds + threadIdx.x / WAVE * 1024);
 #pragma unroll
     for (int u = 0; u < N; ++u) {
-      const char *p = (const char *)base + offset[u];
-      if constexpr (!FULL) {
+      if constexpr (FULL) {
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                     :: "s"(at + NT * 16 * u), "v"(offset[u]), "s"(base) : "memory");
+      } else {
+        const char *p = (const char *)base + offset[u];
         const int e = threadIdx.x + NT * u;
         if ((KC ? 8 * swap(e / CPR, e % CPR) : e / CPR) >= left) p = (const char *)&zero_chunk;
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                     :: "s"(at + NT * 16 * u), "v"(p) : "memory");
       }
-      __builtin_amdgcn_global_load_lds((global_t)p, (lds_t)(lds + NT * 16 * u), 16, 0, 0);
     }
   }
 
@@ -418,8 +423,16 @@ __global__ void __launch_bounds__(256, 2) k_gemm(GemmArgs a) {
   }
 }
 
+// The block's own reads into LDS are done, its waves' reads of LDS too
+__device__ __forceinline__ void arrived() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 // The same for 16-bit operands whose rows lie on 16-byte boundaries: K-tiles go
-// straight from memory into LDS, the next one while this one is multiplied.
+// straight from memory into LDS, two ahead of the products, and from there into
+// registers half a K-tile ahead, so that the matrix cores wait for neither.
 // WI x WJ waves; each reads (TI / WI + TJ / WJ) x 128 bytes of LDS per K-tile for
 // TI / WI x TJ / WJ outputs
 template <class T, int TI, int TJ, int WI, int WJ, bool IK, bool JK, bool LIN>
@@ -429,6 +442,7 @@ __global__ void __launch_bounds__(WI *WJ *WAVE, 2) k_gemm_dma(GemmArgs a) {
   typedef Operand<T, TJ, JK, false, NT> OB;
   constexpr int BK = OA::BK, BUF = OA::BYTES + OB::BYTES;
   __shared__ __attribute__((aligned(16))) char lds[2 * BUF];
+  const uint32_t la = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
   const int wave = threadIdx.x / WAVE;
   const int wi = TI / WI * (wave % WI), wj = TJ / WJ * (wave / WI);
   const int64_t tj = (a.J + TJ - 1) / TJ, tiles = (a.I + TI - 1) / TI * tj;
@@ -445,17 +459,15 @@ __global__ void __launch_bounds__(WI *WJ *WAVE, 2) k_gemm_dma(GemmArgs a) {
     const T *pa = (const T *)a.A.p + (IK ? i0 * a.A.ld + k0 : k0 * a.A.ld + i0);
     const T *pb = (const T *)a.B.p + (JK ? j0 * a.B.ld + k0 : k0 * a.B.ld + j0);
     const int64_t sa = IK ? BK : BK * a.A.ld, sb = JK ? BK : BK * a.B.ld;
-    auto fetch = [&](int64_t k, int buf) {
-      char *da = lds + buf * BUF, *db = da + OA::BYTES;
-      if (k + BK <= k1) {
-        OA::template dma<true>(pa, oa, da, BK);
-        OB::template dma<true>(pb, ob, db, BK);
-      } else {   // the last, short one
-        OA::template dma<false>(pa, oa, da, (int)(k1 - k));
-        OB::template dma<false>(pb, ob, db, (int)(k1 - k));
-      }
+    auto fetch = [&](auto full, int buf, int left) {
+      OA::template dma<decltype(full)::value>(pa, oa, la + buf * BUF, left);
+      OB::template dma<decltype(full)::value>(pb, ob, la + buf * BUF + OA::BYTES, left);
       pa += sa;
       pb += sb;
+    };
+    auto fetch_any = [&](int buf, int64_t left) {   // 0 < left
+      if (left >= BK) fetch(std::true_type{}, buf, BK);
+      else fetch(std::false_type{}, buf, (int)left);
     };
     v4f acc[NI][NJ];
 #pragma unroll
@@ -463,13 +475,49 @@ __global__ void __launch_bounds__(WI *WJ *WAVE, 2) k_gemm_dma(GemmArgs a) {
 #pragma unroll
       for (int j = 0; j < NJ; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
     __syncthreads();   // the tile before has been read
-    if (k0 < k1) fetch(k0, 0);
-    int buf = 0;
-    for (int64_t k = k0; k < k1; k += BK, buf ^= 1) {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();
-      if (k + BK < k1) fetch(k + BK, buf ^ 1);
-      multiply<OA, OB>(lds + buf * BUF, lds + buf * BUF + OA::BYTES, wi, wj, acc);
+    if (k0 < k1) {
+      typename OA::E8 fi[2][NI], fj[2][NJ];   // the operands of a K-tile's two halves
+      auto read = [&](int half, int buf) {
+        const char *da = lds + buf * BUF, *db = da + OA::BYTES;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) fj[half][j] = OB::frag(db, 0, wj + 16 * j, half);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) fi[half][i] = OA::frag(da, 0, wi + 16 * i, half);
+      };
+      auto multiply = [&](int half) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) acc[i][j] = mma(fj[half][j], fi[half][i], acc[i][j]);
+      };
+      fetch_any(0, k1 - k0);
+      arrived();
+      if (k0 + BK < k1) fetch_any(1, k1 - k0 - BK);
+      read(0, 0);
+      int buf = 0;
+      int64_t k = k0;
+      for (; k + 3 * BK <= k1; k += BK, buf ^= 1) {
+        read(1, buf);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(0);
+        __builtin_amdgcn_sched_barrier(0);
+        arrived();   // the next K-tile is there, and this one has been read
+        fetch(std::true_type{}, buf, BK);
+        read(0, buf ^ 1);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(1);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      for (; k < k1; k += BK, buf ^= 1) {   // the last ones
+        read(1, buf);
+        multiply(0);
+        if (k + BK < k1) {
+          arrived();
+          if (k + 2 * BK < k1) fetch_any(buf, k1 - k - 2 * BK);
+        }
+        multiply(1);
+        if (k + BK < k1) read(0, buf ^ 1);
+      }
     }
     __syncthreads();   // the last K-tile has been read
     constexpr int MINE = sizeof lds / (WI * WJ);
