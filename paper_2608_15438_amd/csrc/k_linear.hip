@@ -109,11 +109,11 @@ __device__ const uint4 zero_chunk = {0, 0, 0, 0};
 //     exchanged by k, and a block is read transposed (ds_read_b64_tr_b16: sixteen
 //     lanes give the addresses of four rows of sixteen columns, and lane t
 //     receives the four elements of column t).
-template <class T, int R, bool KC, bool HELD, int NT = 256>
+template <class T, int R, bool KC, bool HELD, int NT = 256, int BK_ = Tile<T>::BK>
 struct Operand {
   typedef typename Tile<T>::E E;
   typedef E E8 __attribute__((ext_vector_type(8)));
-  static constexpr int BK = Tile<T>::BK, P = Tile<T>::P;
+  static constexpr int BK = BK_, P = Tile<T>::P;
   static constexpr int N = R * BK / 8 / NT;       // chunks per thread
   static constexpr int CPR = (KC ? BK : R) / 8;   // chunks per row of the tile in memory
   static constexpr int PLANE = R * BK * 2, BYTES = P * PLANE;
@@ -423,28 +423,21 @@ __global__ void __launch_bounds__(256, 2) k_gemm(GemmArgs a) {
   }
 }
 
-// The block's own reads into LDS are done, its waves' reads of LDS too
-__device__ __forceinline__ void arrived() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
-}
-
 // The same for 16-bit operands whose rows lie on 16-byte boundaries: K-tiles go
-// straight from memory into LDS, two ahead of the products, and from there into
-// registers half a K-tile ahead, so that the matrix cores wait for neither.
-// WI x WJ waves; each reads (TI / WI + TJ / WJ) x 128 bytes of LDS per K-tile for
-// TI / WI x TJ / WJ outputs
-template <class T, int TI, int TJ, int WI, int WJ, bool IK, bool JK, bool LIN>
-__global__ void __launch_bounds__(WI *WJ *WAVE, 2) k_gemm_dma(GemmArgs a) {
-  constexpr int NT = WI * WJ * WAVE, NI = TI / WI / 16, NJ = TJ / WJ / 16;
-  typedef Operand<T, TI, IK, false, NT> OA;
-  typedef Operand<T, TJ, JK, false, NT> OB;
-  constexpr int BK = OA::BK, BUF = OA::BYTES + OB::BYTES;
-  __shared__ __attribute__((aligned(16))) char lds[2 * BUF];
+// straight from memory into LDS, two ahead of the products.  256 x 128 tiles by
+// four waves: two blocks share a CU, and one reads its operands from LDS, or makes
+// its epilogue, while the other multiplies
+template <class T, int TI, int TJ, bool IK, bool JK, bool LIN>
+__global__ void __launch_bounds__(256, 2) k_gemm_dma(GemmArgs a) {
+  constexpr int BK = 32, NB = 3, NI = TI / 32, NJ = TJ / 32;
+  typedef Operand<T, TI, IK, false, 256, BK> OA;
+  typedef Operand<T, TJ, JK, false, 256, BK> OB;
+  typedef typename OA::E8 E8;
+  constexpr int BUF = OA::BYTES + OB::BYTES;
+  __shared__ __attribute__((aligned(16))) char lds[NB * BUF];
   const uint32_t la = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
   const int wave = threadIdx.x / WAVE;
-  const int wi = TI / WI * (wave % WI), wj = TJ / WJ * (wave / WI);
+  const int wi = TI / 2 * (wave & 1), wj = TJ / 2 * (wave >> 1);
   const int64_t tj = (a.J + TJ - 1) / TJ, tiles = (a.I + TI - 1) / TI * tj;
   const int64_t per = (tiles + 7) / 8;
   const int64_t k0 = (int64_t)blockIdx.y * a.kchunk;
@@ -459,68 +452,64 @@ __global__ void __launch_bounds__(WI *WJ *WAVE, 2) k_gemm_dma(GemmArgs a) {
     const T *pa = (const T *)a.A.p + (IK ? i0 * a.A.ld + k0 : k0 * a.A.ld + i0);
     const T *pb = (const T *)a.B.p + (JK ? j0 * a.B.ld + k0 : k0 * a.B.ld + j0);
     const int64_t sa = IK ? BK : BK * a.A.ld, sb = JK ? BK : BK * a.B.ld;
-    auto fetch = [&](auto full, int buf, int left) {
-      OA::template dma<decltype(full)::value>(pa, oa, la + buf * BUF, left);
-      OB::template dma<decltype(full)::value>(pb, ob, la + buf * BUF + OA::BYTES, left);
-      pa += sa;
-      pb += sb;
-    };
-    auto fetch_any = [&](int buf, int64_t left) {   // 0 < left
-      if (left >= BK) fetch(std::true_type{}, buf, BK);
-      else fetch(std::false_type{}, buf, (int)left);
-    };
     v4f acc[NI][NJ];
 #pragma unroll
     for (int i = 0; i < NI; ++i)
 #pragma unroll
       for (int j = 0; j < NJ; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
+    int in = 0, out = 0;        // LDS buffers to fill and to read next
+    int64_t left = k1 - k0;     // of k, not yet asked for
+    auto next = [](int &b) { b = b == (NB - 1) * BUF ? 0 : b + BUF; };
+    auto fetch = [&](auto full) {
+      OA::template dma<decltype(full)::value>(pa, oa, la + in, (int)left);
+      OB::template dma<decltype(full)::value>(pb, ob, la + in + OA::BYTES, (int)left);
+      pa += sa;
+      pb += sb;
+      left -= BK;
+      next(in);
+    };
+    auto fetch_any = [&]() {
+      if (left >= BK) fetch(std::true_type{});
+      else if (left > 0) fetch(std::false_type{});
+    };
+    auto multiply = [&]() {
+      E8 fi[NI], fj[NJ];
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) fj[j] = OB::frag(lds + out + OA::BYTES, 0, wj + 16 * j, 0);
+#pragma unroll
+      for (int i = 0; i < NI; ++i) fi[i] = OA::frag(lds + out, 0, wi + 16 * i, 0);
+      next(out);
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[i][j] = mma(fj[j], fi[i], acc[i][j]);
+    };
+    // the wave's own reads into LDS are done but for the last `but`, its reads of
+    // LDS too; then the other waves' as well
+    auto arrived = [](auto but) {
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(decltype(but)::value) : "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+    };
+    std::integral_constant<int, 0> ALL;
+    std::integral_constant<int, OA::N + OB::N> BUT_LAST;
     __syncthreads();   // the tile before has been read
-    if (k0 < k1) {
-      typename OA::E8 fi[2][NI], fj[2][NJ];   // the operands of a K-tile's two halves
-      auto read = [&](int half, int buf) {
-        const char *da = lds + buf * BUF, *db = da + OA::BYTES;
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) fj[half][j] = OB::frag(db, 0, wj + 16 * j, half);
-#pragma unroll
-        for (int i = 0; i < NI; ++i) fi[half][i] = OA::frag(da, 0, wi + 16 * i, half);
-      };
-      auto multiply = [&](int half) {
-#pragma unroll
-        for (int i = 0; i < NI; ++i)
-#pragma unroll
-          for (int j = 0; j < NJ; ++j) acc[i][j] = mma(fj[half][j], fi[half][i], acc[i][j]);
-      };
-      fetch_any(0, k1 - k0);
-      arrived();
-      if (k0 + BK < k1) fetch_any(1, k1 - k0 - BK);
-      read(0, 0);
-      int buf = 0;
-      int64_t k = k0;
-      for (; k + 3 * BK <= k1; k += BK, buf ^= 1) {
-        read(1, buf);
-        __builtin_amdgcn_sched_barrier(0);
-        multiply(0);
-        __builtin_amdgcn_sched_barrier(0);
-        arrived();   // the next K-tile is there, and this one has been read
-        fetch(std::true_type{}, buf, BK);
-        read(0, buf ^ 1);
-        __builtin_amdgcn_sched_barrier(0);
-        multiply(1);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      for (; k < k1; k += BK, buf ^= 1) {   // the last ones
-        read(1, buf);
-        multiply(0);
-        if (k + BK < k1) {
-          arrived();
-          if (k + 2 * BK < k1) fetch_any(buf, k1 - k - 2 * BK);
-        }
-        multiply(1);
-        if (k + BK < k1) read(0, buf ^ 1);
-      }
+    const int64_t nk = (k1 - k0 + BK - 1) / BK;
+    fetch_any();
+    fetch_any();
+    int64_t n = 0;
+    for (; left >= BK; ++n) {   // while a whole K-tile can be asked for
+      arrived(BUT_LAST);
+      fetch(std::true_type{});
+      multiply();
+    }
+    for (; n < nk; ++n) {       // the last ones
+      arrived(ALL);
+      fetch_any();
+      multiply();
     }
     __syncthreads();   // the last K-tile has been read
-    constexpr int MINE = sizeof lds / (WI * WJ);
+    constexpr int MINE = sizeof lds / 4;
     write_tile<T, NI, NJ, MINE, IK, JK, false, LIN>(a, acc, lds + wave * MINE, i0 + wi, j0 + wj,
                                                     k0, k1);
   }
@@ -605,7 +594,7 @@ struct Split {
 static Split split_of(int64_t I, int J, int64_t K, int dtype) {
   auto tiles = [&](int64_t t) { return up(I, t) / t * (up(J, t) / t); };
   Split sp{128, 1, 64};
-  if (dtype != NR_F32 && tiles(256) >= 256) sp.side = 256;
+  if (dtype != NR_F32 && tiles(256) >= 256) sp.side = 256;   // 256 x 128
   else if (tiles(128) < 256 && tiles(128) * (K / 512) < 256) sp.side = 64;
   const int64_t n = tiles(sp.side);
   int64_t parts = n > 0 && n < 256 ? (512 + n - 1) / n : 1;
@@ -638,10 +627,9 @@ static void gemm_tiles(const GemmArgs &a, int parts, hipStream_t s) {
   const dim3 g((unsigned)(tiles < 1 << 22 ? tiles : 1 << 22), parts);
   if constexpr (sizeof(T) == 2 && S >= 128) {
     if (direct(a.A, IK ? a.K : a.I) && direct(a.B, JK ? a.K : a.J)) {
-      if constexpr (S == 256)
-        hipLaunchKernelGGL((k_gemm_dma<T, S, S, 2, 4, IK, JK, LIN>), g, dim3(512), 0, s, a);
-      else
-        hipLaunchKernelGGL((k_gemm_dma<T, S, S, 2, 2, IK, JK, LIN>), g, dim3(256), 0, s, a);
+      const int64_t n = up(up(a.I, S) / S * (up(a.J, 128) / 128), 8);
+      hipLaunchKernelGGL((k_gemm_dma<T, S, 128, IK, JK, LIN>),
+                         dim3((unsigned)(n < 1 << 22 ? n : 1 << 22), parts), dim3(256), 0, s, a);
       return;
     }
   }
