@@ -28,24 +28,23 @@ struct GemmArgs {
   LinearArgs lin;
 };
 
-// The epilogue of eight columns of a row from j on (a multiple of 8).  A group held
-// in 8 bits lies in the lanes of a quad, which call it together; ok: the row is
-// inside
+// The epilogue of eight columns of a row from j on (a multiple of 8), with their
+// bias and residual.  A group held in 8 bits lies in the lanes of a quad, which
+// call it together; ok: the row is inside
 template <class T, bool LIN>
 __device__ __forceinline__ void finish(const GemmArgs &a, int64_t i, int j, bool ok,
-                                       float (&v)[8]) {
+                                       float (&v)[8], const Raw8<T> &bias, const Raw8<T> &res) {
   if constexpr (!LIN) {
     if (ok) store8((T *)a.out + i * a.ldo, j, a.J, v);
   } else {
     constexpr bool exact = sizeof(T) == 4;
     const LinearArgs &l = a.lin;
-    float u[8];
     if (l.bias) {
-      load8((const T *)l.bias, j, a.J, u);
 #pragma unroll
-      for (int r = 0; r < 8; ++r) v[r] += u[r];
+      for (int r = 0; r < 8; ++r) v[r] += bias[r];
     }
     if (l.pre_hold) {
+      float u[8];
 #pragma unroll
       for (int r = 0; r < 8; ++r) u[r] = j + r < a.J ? to_f32(from_f32<T>(v[r])) : 0.0f;
       if (ok && j < l.ldp)   // the rows of q are whole groups, so a quad is in or out
@@ -58,9 +57,8 @@ __device__ __forceinline__ void finish(const GemmArgs &a, int64_t i, int j, bool
 #pragma unroll
     for (int r = 0; r < 8; ++r) v[r] = act_value<exact>(v[r], l.act);
     if (l.res) {
-      load8((const T *)l.res + i * l.ldr, j, a.J, u);
 #pragma unroll
-      for (int r = 0; r < 8; ++r) v[r] += u[r];
+      for (int r = 0; r < 8; ++r) v[r] += res[r];
     }
     store8((T *)l.y + i * l.ldy, j, a.J, v);
   }
@@ -278,43 +276,65 @@ __device__ float plain_chain(const LayerMat &A, const LayerMat &B, int64_t i, in
   return s;
 }
 
-// A wave's outputs, rows i0.. and columns j0.., or their parts' sums, by way of LDS:
-// there a lane has four columns of a row in each block, and eight neighbouring
-// ones for the epilogue, so that a row's outputs are written whole.  lds: BYTES
-// of the wave's own; the chunks of four floats are exchanged by the row's number
-// against bank conflicts
-template <class T, int NI, int NJ, int BYTES, bool IK, bool JK, bool HELD, bool LIN>
+// A wave's outputs, rows i0.. and columns j0.., or their parts' sums, sixteen rows at
+// a time by way of LDS: there a lane has four columns of a row in each block,
+// and eight neighbouring ones for the epilogue, so that a row's outputs are
+// written whole.  The residual of the next rows is asked for before these are
+// finished.  lds: the wave's own 1 KB per block of columns; the chunks of four
+// floats are exchanged by the row's number against bank conflicts
+template <class T, int NI, int NJ, bool IK, bool JK, bool HELD, bool LIN>
 __device__ __forceinline__ void write_tile(const GemmArgs &a, const v4f (&acc)[NI][NJ], char *lds,
                                            int64_t i0, int64_t j0, int64_t k0, int64_t k1) {
   constexpr int W = 16 * NJ, CH = W / 4, LPR = W / 8;    // columns, chunks and lanes of a row
-  constexpr int FIT = BYTES / (16 * W * 4);              // blocks of rows that fit
-  constexpr int NB = FIT >= NI ? NI : FIT >= 4 ? 4 : FIT >= 2 ? 2 : 1;
-  static_assert(FIT >= 1 && NI % NB == 0, "whole passes");
-  const int lane = lane_id();
+  constexpr int RPS = WAVE / LPR, NS = 16 / RPS;         // rows per step, steps
+  const int lane = threadIdx.x & (WAVE - 1), c = 2 * (lane % LPR);
+  const int64_t j = j0 + 4 * c;
   float4 *buf = reinterpret_cast<float4 *>(lds);
+  const bool inner = j < a.J;
+  Raw8<T> bias, res[2][NS];
+  auto residual = [&](int p) {
+    if constexpr (LIN)
+      if (a.lin.res)
 #pragma unroll
-  for (int p = 0; p < NI; p += NB) {
+        for (int s = 0; s < NS; ++s) {
+          const int64_t i = i0 + 16 * p + s * RPS + lane / LPR;
+          if (i < a.I && inner)
+            res[p & 1][s].load((const T *)a.lin.res + i * a.lin.ldr, (int)j, a.J);
+        }
+  };
+  if constexpr (LIN)
+    if (a.lin.bias) bias.load((const T *)a.lin.bias, (int)j, a.J);
+  residual(0);
 #pragma unroll
-    for (int i = 0; i < NB; ++i)
+  for (int p = 0; p < NI; ++p) {
+    if (p + 1 < NI) residual(p + 1);
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) {
-        const int row = 16 * i + (lane & 15), c = 4 * j + (lane >> 4);
-        const v4f v = acc[p + i][j];
-        buf[row * CH + (c ^ (row & 7))] = make_float4(v[0], v[1], v[2], v[3]);
-      }
+    for (int b = 0; b < NJ; ++b) {
+      const int row = lane & 15, ch = 4 * b + (lane >> 4);
+      buf[row * CH + (ch ^ (row & 7))] =
+          make_float4(acc[p][b][0], acc[p][b][1], acc[p][b][2], acc[p][b][3]);
+    }
     // a wave's LDS accesses are carried out in order
     __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-    for (int s = 0; s < NB * 16 * LPR / WAVE; ++s) {
-      const int row = s * (WAVE / LPR) + lane / LPR, c = 2 * (lane % LPR);
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      const int row = s * RPS + lane / LPR;
       const float4 x = buf[row * CH + (c ^ (row & 7))], y = buf[row * CH + ((c + 1) ^ (row & 7))];
       float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-      const int64_t i = i0 + 16 * p + row, j = j0 + 4 * c;
+      const int64_t i = i0 + 16 * p + row;
       if constexpr (sizeof(T) == 4) {
+        bool bad = false;
 #pragma unroll
-        for (int r = 0; r < 8; ++r)
-          if (!(fabsf(v[r]) < INFINITY) && i < a.I && j + r < a.J)
-            v[r] = plain_chain<IK, JK, HELD>(a.A, a.B, i, (int)j + r, k0, k1);
+        for (int r = 0; r < 8; ++r) bad = bad || !(fabsf(v[r]) < INFINITY);
+        if (bad && i < a.I) {
+#pragma unroll 1
+          for (int r = 0; r < 8; ++r)
+            if (j + r < a.J) {
+              const float o = plain_chain<IK, JK, HELD>(a.A, a.B, i, (int)j + r, k0, k1);
+#pragma unroll
+              for (int q = 0; q < 8; ++q) v[q] = q == r ? o : v[q];
+            }
+        }
       }
       if (a.part) {
         if (i < a.I && j < a.ldp) {
@@ -323,11 +343,20 @@ __device__ __forceinline__ void write_tile(const GemmArgs &a, const v4f (&acc)[N
           o[1] = make_float4(v[4], v[5], v[6], v[7]);
         }
       } else {
-        finish<T, LIN>(a, i, (int)j, i < a.I, v);
+        finish<T, LIN>(a, i, (int)j, i < a.I, v, bias, res[p & 1][s]);
       }
     }
     __builtin_amdgcn_wave_barrier();
   }
+}
+
+// Which tile comes t-th: groups of eight rows of tiles, a group's tiles column by
+// column, so that the tiles that are worked on together need few distinct rows of
+// either operand (64 tiles: 8 by 8)
+__device__ __forceinline__ void tile_at(int64_t t, int64_t ti, int64_t tj, int64_t &i, int64_t &j) {
+  const int64_t g = t / (8 * tj), r = t - g * 8 * tj, h = ti - 8 * g < 8 ? ti - 8 * g : 8;
+  j = r / h;
+  i = 8 * g + r - j * h;
 }
 
 // The products of a K-tile in LDS
@@ -369,14 +398,16 @@ __global__ void __launch_bounds__(256, 2) k_gemm(GemmArgs a) {
   __shared__ __attribute__((aligned(16))) char lds[NBUF][OA::BYTES + OB::BYTES];
   const int lane = lane_id(), wave = threadIdx.x / WAVE;
   const int wi = TI / 2 * (wave & 1), wj = TJ / 2 * (wave >> 1);
-  const int64_t tj = (a.J + TJ - 1) / TJ, tiles = (a.I + TI - 1) / TI * tj;
+  const int64_t ti = (a.I + TI - 1) / TI, tj = (a.J + TJ - 1) / TJ, tiles = ti * tj;
   const int64_t per = (tiles + 7) / 8;
   const int64_t k0 = (int64_t)blockIdx.y * a.kchunk;
   const int64_t k1 = k0 + a.kchunk < a.K ? k0 + a.kchunk : a.K;
   for (int64_t u = blockIdx.x; u < 8 * per; u += gridDim.x) {
     const int64_t t = (u & 7) * per + (u >> 3);
     if (t >= tiles) continue;   // the whole block together
-    const int64_t i0 = t / tj * TI, j0 = t % tj * TJ;
+    int64_t i0, j0;
+    tile_at(t, ti, tj, i0, j0);
+    i0 *= TI, j0 *= TJ;
     const bool inside = i0 + TI <= a.I && j0 + TJ <= a.J;
     OA fa;
     OB fb;
@@ -417,9 +448,8 @@ __global__ void __launch_bounds__(256, 2) k_gemm(GemmArgs a) {
       }
     }
     __syncthreads();   // the last K-tile has been read
-    constexpr int MINE = sizeof lds / 4;
-    write_tile<T, NI, NJ, MINE, IK, JK, HELD, LIN>(a, acc, (char *)lds + wave * MINE, i0 + wi,
-                                                   j0 + wj, k0, k1);
+    write_tile<T, NI, NJ, IK, JK, HELD, LIN>(a, acc, (char *)lds + wave * 1024 * NJ, i0 + wi,
+                                             j0 + wj, k0, k1);
   }
 }
 
@@ -438,40 +468,63 @@ __global__ void __launch_bounds__(256, 2) k_gemm_dma(GemmArgs a) {
   const uint32_t la = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
   const int wave = threadIdx.x / WAVE;
   const int wi = TI / 2 * (wave & 1), wj = TJ / 2 * (wave >> 1);
-  const int64_t tj = (a.J + TJ - 1) / TJ, tiles = (a.I + TI - 1) / TI * tj;
+  const int64_t ti = (a.I + TI - 1) / TI, tj = (a.J + TJ - 1) / TJ, tiles = ti * tj;
   const int64_t per = (tiles + 7) / 8;
   const int64_t k0 = (int64_t)blockIdx.y * a.kchunk;
   const int64_t k1 = k0 + a.kchunk < a.K ? k0 + a.kchunk : a.K;
-  for (int64_t u = blockIdx.x; u < 8 * per; u += gridDim.x) {
-    const int64_t t = (u & 7) * per + (u >> 3);
-    if (t >= tiles) continue;   // the whole block together
-    const int64_t i0 = t / tj * TI, j0 = t % tj * TJ;
-    uint32_t oa[OA::N], ob[OB::N];
-    OA::dma_offsets(a.A, i0, a.I, oa);
-    OB::dma_offsets(a.B, j0, a.J, ob);
-    const T *pa = (const T *)a.A.p + (IK ? i0 * a.A.ld + k0 : k0 * a.A.ld + i0);
-    const T *pb = (const T *)a.B.p + (JK ? j0 * a.B.ld + k0 : k0 * a.B.ld + j0);
-    const int64_t sa = IK ? BK : BK * a.A.ld, sb = JK ? BK : BK * a.B.ld;
+  int in = 0, out = 0;          // LDS buffers to fill and to read next
+  int64_t i0 = 0, j0 = 0, left = 0;   // the tile; k of it not yet asked for
+  uint32_t oa[OA::N], ob[OB::N];
+  const T *pa = nullptr, *pb = nullptr;
+  const int64_t sa = IK ? BK : BK * a.A.ld, sb = JK ? BK : BK * a.B.ld;
+  auto next = [](int &b) { b = b == (NB - 1) * BUF ? 0 : b + BUF; };
+  auto fetch = [&](auto full) {
+    OA::template dma<decltype(full)::value>(pa, oa, la + in, (int)left);
+    OB::template dma<decltype(full)::value>(pb, ob, la + in + OA::BYTES, (int)left);
+    pa += sa;
+    pb += sb;
+    left -= BK;
+    next(in);
+  };
+  auto fetch_any = [&]() {
+    if (left >= BK) fetch(std::true_type{});
+    else if (left > 0) fetch(std::false_type{});
+  };
+  // the block's next tile from its u-th on (-1: none left), its first two K-tiles
+  // asked for
+  auto begin = [&](int64_t u) -> int64_t {
+    for (; u < 8 * per; u += gridDim.x)
+      if ((u & 7) * per + (u >> 3) < tiles) {
+        tile_at((u & 7) * per + (u >> 3), ti, tj, i0, j0);
+        i0 *= TI, j0 *= TJ;
+        OA::dma_offsets(a.A, i0, a.I, oa);
+        OB::dma_offsets(a.B, j0, a.J, ob);
+        pa = (const T *)a.A.p + (IK ? i0 * a.A.ld + k0 : k0 * a.A.ld + i0);
+        pb = (const T *)a.B.p + (JK ? j0 * a.B.ld + k0 : k0 * a.B.ld + j0);
+        left = k1 - k0;
+        fetch_any();
+        fetch_any();
+        return u;
+      }
+    return -1;
+  };
+  // the wave's own reads into LDS are done but for the last `but`, its reads of
+  // LDS too; then the other waves' as well
+  auto arrived = [](auto but) {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(decltype(but)::value) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  std::integral_constant<int, 0> ALL;
+  std::integral_constant<int, OA::N + OB::N> BUT_LAST;
+  const int64_t nk = (k1 - k0 + BK - 1) / BK;
+  int64_t u = begin(blockIdx.x);
+  while (u >= 0) {
     v4f acc[NI][NJ];
 #pragma unroll
     for (int i = 0; i < NI; ++i)
 #pragma unroll
       for (int j = 0; j < NJ; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
-    int in = 0, out = 0;        // LDS buffers to fill and to read next
-    int64_t left = k1 - k0;     // of k, not yet asked for
-    auto next = [](int &b) { b = b == (NB - 1) * BUF ? 0 : b + BUF; };
-    auto fetch = [&](auto full) {
-      OA::template dma<decltype(full)::value>(pa, oa, la + in, (int)left);
-      OB::template dma<decltype(full)::value>(pb, ob, la + in + OA::BYTES, (int)left);
-      pa += sa;
-      pb += sb;
-      left -= BK;
-      next(in);
-    };
-    auto fetch_any = [&]() {
-      if (left >= BK) fetch(std::true_type{});
-      else if (left > 0) fetch(std::false_type{});
-    };
     auto multiply = [&]() {
       E8 fi[NI], fj[NJ];
 #pragma unroll
@@ -484,34 +537,25 @@ __global__ void __launch_bounds__(256, 2) k_gemm_dma(GemmArgs a) {
 #pragma unroll
         for (int j = 0; j < NJ; ++j) acc[i][j] = mma(fj[j], fi[i], acc[i][j]);
     };
-    // the wave's own reads into LDS are done but for the last `but`, its reads of
-    // LDS too; then the other waves' as well
-    auto arrived = [](auto but) {
-      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(decltype(but)::value) : "memory");
-      __builtin_amdgcn_s_barrier();
-      asm volatile("" ::: "memory");
-    };
-    std::integral_constant<int, 0> ALL;
-    std::integral_constant<int, OA::N + OB::N> BUT_LAST;
-    __syncthreads();   // the tile before has been read
-    const int64_t nk = (k1 - k0 + BK - 1) / BK;
-    fetch_any();
-    fetch_any();
     int64_t n = 0;
-    for (; left >= BK; ++n) {   // while a whole K-tile can be asked for
+    while (left >= BK) {   // a whole K-tile is still to be asked for
       arrived(BUT_LAST);
       fetch(std::true_type{});
       multiply();
+      ++n;
     }
-    for (; n < nk; ++n) {       // the last ones
+    for (; n < nk; ++n) {   // the last ones
       arrived(ALL);
       fetch_any();
       multiply();
     }
-    __syncthreads();   // the last K-tile has been read
-    constexpr int MINE = sizeof lds / 4;
-    write_tile<T, NI, NJ, MINE, IK, JK, false, LIN>(a, acc, lds + wave * MINE, i0 + wi, j0 + wj,
-                                                    k0, k1);
+    arrived(ALL);   // the last K-tile has been read
+    // the next tile's first K-tiles come while this one is finished; the third
+    // buffer is free for that
+    const int64_t i1 = i0 + wi, j1 = j0 + wj;
+    u = begin(u + gridDim.x);
+    write_tile<T, NI, NJ, IK, JK, false, LIN>(a, acc, lds + in + wave * 1024 * NJ, i1, j1, k0, k1);
+    __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): nothing is under way into registers
   }
 }
 
@@ -524,6 +568,11 @@ __global__ void __launch_bounds__(256) k_gemm_join(GemmArgs a, int parts) {
     const int64_t i = u / per;
     const int j = (int)(u - i * per) * 8;
     float v[8] = {};
+    Raw8<T> bias, res;
+    if constexpr (LIN) {
+      if (a.lin.bias) bias.load((const T *)a.lin.bias, j, a.J);
+      if (a.lin.res) res.load((const T *)a.lin.res + i * a.lin.ldr, j, a.J);
+    }
     for (int s = 0; s < parts; ++s) {
       const float4 *p =
           reinterpret_cast<const float4 *>(a.part + ((int64_t)s * a.I + i) * a.ldp + j);
@@ -531,7 +580,7 @@ __global__ void __launch_bounds__(256) k_gemm_join(GemmArgs a, int parts) {
       v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
       v[4] += y.x, v[5] += y.y, v[6] += y.z, v[7] += y.w;
     }
-    finish<T, LIN>(a, i, j, true, v);
+    finish<T, LIN>(a, i, j, true, v, bias, res);
   }
 }
 
@@ -628,8 +677,9 @@ static void gemm_tiles(const GemmArgs &a, int parts, hipStream_t s) {
   if constexpr (sizeof(T) == 2 && S >= 128) {
     if (direct(a.A, IK ? a.K : a.I) && direct(a.B, JK ? a.K : a.J)) {
       const int64_t n = up(up(a.I, S) / S * (up(a.J, 128) / 128), 8);
+      const int64_t room = up(512 / parts > 0 ? 512 / parts : 1, 8);   // two blocks a CU
       hipLaunchKernelGGL((k_gemm_dma<T, S, 128, IK, JK, LIN>),
-                         dim3((unsigned)(n < 1 << 22 ? n : 1 << 22), parts), dim3(256), 0, s, a);
+                         dim3((unsigned)(n < room ? n : room), parts), dim3(256), 0, s, a);
       return;
     }
   }
