@@ -101,8 +101,9 @@ __device__ const uint4 zero_chunk = {0, 0, 0, 0};
 // (16 bytes of LDS), read from memory into registers and, a K-tile later, put
 // into LDS.
 //   KC (k along the operand's rows): [R][BK]; the chunks of a row are exchanged
-//     by the row's number, so that the sixteen rows that a matrix instruction
-//     reads at one k lie on different banks.
+//     by the row's number, so that the lanes that LDS serves together (a quarter
+//     of a wave, by fours: 0-3, 12-15, 20-23, 24-27, and so on) find theirs on
+//     different banks.
 //   otherwise: [BK][R]; pairs of chunks (the sixteen columns of a block) are
 //     exchanged by k, and a block is read transposed (ds_read_b64_tr_b16: sixteen
 //     lanes give the addresses of four rows of sixteen columns, and lane t
@@ -125,7 +126,7 @@ struct Operand {
   // chunk that lies at place c
   static __device__ __forceinline__ int swap(int row, int c) {
     if constexpr (KC && BK == 64) return c ^ (row & 7);
-    else if constexpr (KC) return c ^ (((row >> 2) & 1) | ((((row >> 1) ^ (row >> 3)) & 1) << 1));
+    else if constexpr (KC) return c ^ ((row >> 3) & 1) << 1;
     else if constexpr (R >= 128) return c ^ (((row & 3) | ((row >> 3) & 1) << 2) << 1);
     else return c ^ ((row & 3) << 1);
   }
