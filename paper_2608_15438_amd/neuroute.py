@@ -412,6 +412,8 @@ def _mat(t, name, dtype, device, m=None, w=None):
                          f"got {list(t.shape)}")
     if not t.is_cuda or t.dtype != dtype or t.device != device:
         raise ValueError(f"{name} must be {dtype} on {device}, got {t.dtype} on {t.device}")
+    if t.numel() == 0:
+        return t.data_ptr(), t.shape[1]
     if t.shape[1] > 1 and t.stride(1) != 1:
         raise ValueError(f"{name}: the elements of a row must be next to each other")
     ld = t.stride(0)

@@ -3,7 +3,9 @@ Eq. similarityconfig and the mask of Eq. 8), untimed.  On the GPU the
 pairwise input distances run on the library's fp32 matrix-core kernel
 (nr_pair_sqdist) and the loss, mask and latent gradient in one fused pass
 over the pairs (nr_lsim_grad); the encoder's own layers are torch Linear
-modules.  lsim_loss below is the same loss in PyTorch (CPU checks).
+modules, or with layers="hip" the library's (nr_linear and its gradients), in
+fp32, bf16 or fp16 and with their activations in 8 bits if asked for.
+lsim_loss below is the same loss in PyTorch (CPU checks).
 
 For a mini-batch of B rows x (scaled as the encoder sees them) and their
 latents l, with rho = sqrt(L_dim / E_dim):
@@ -105,10 +107,20 @@ def lsim_loss_gpu(x: torch.Tensor, lat: torch.Tensor, gamma: float,
 
 class _Mlp(torch.nn.Module):
     """The encoder as trainable fp32 layers (ReLU between layers, the input
-    scaled as at query time)."""
+    scaled as at query time).  layers="hip" runs them on the library's kernels,
+    in `dtype` (the parameters and the latents stay fp32) and with the activations
+    kept for the backward pass in 8 bits if `hold` says so."""
 
-    def __init__(self, enc: Encoder, device):
+    def __init__(self, enc: Encoder, device, layers: str = "torch", dtype=torch.float32,
+                 hold: Optional[str] = None):
         super().__init__()
+        if layers not in ("torch", "hip"):
+            raise ValueError(f"layers must be 'torch' or 'hip', got {layers!r}")
+        if layers == "torch" and (dtype != torch.float32 or hold is not None):
+            raise ValueError("dtype and hold need layers='hip'")
+        if layers == "hip" and torch.device(device).type != "cuda":
+            raise ValueError("layers='hip' needs a HIP device")
+        self.layers, self.dtype, self.hold = layers, dtype, hold
         self.scale = enc.input_scale
         self.lin = torch.nn.ModuleList()
         for W, b in zip(enc.weights, enc.biases):
@@ -121,6 +133,13 @@ class _Mlp(torch.nn.Module):
 
     def forward(self, x):
         h = x * self.scale
+        if self.layers == "hip":
+            from . import layers as LY
+            h = h.to(self.dtype)
+            for i, l in enumerate(self.lin):
+                h = LY.linear(h, l.weight.to(self.dtype), l.bias.to(self.dtype),
+                              act="relu" if i + 1 < len(self.lin) else "none", hold=self.hold)
+            return h.float()
         for i, l in enumerate(self.lin):
             h = l(h)
             if i + 1 < len(self.lin):
@@ -134,11 +153,15 @@ class _Mlp(torch.nn.Module):
 
 def train_encoder(enc: Encoder, rows_fn: Callable, n: int, steps: int, batch: int = 4096,
                   lr: float = 2e-4, gamma: float = 0.6, tau_emb: Optional[float] = None,
-                  quantile: float = 0.005, seed: int = 0, device="cuda", log=None) -> Encoder:
+                  quantile: float = 0.005, seed: int = 0, device="cuda", log=None,
+                  layers: str = "torch", dtype=torch.float32,
+                  hold: Optional[str] = None) -> Encoder:
     """Adam on L_sim over seeded batches of rows drawn from [0, n) (the
-    encoder has no BatchNorm; its biases and weights are trained)."""
+    encoder has no BatchNorm; its biases and weights are trained).  layers="hip"
+    runs the layers on the library's kernels in `dtype`, with the activations
+    held in 8 bits between the passes for hold="i8" or "e4m3"."""
     dev = torch.device(device)
-    net = _Mlp(enc, dev)
+    net = _Mlp(enc, dev, layers, dtype, hold)
     opt = torch.optim.Adam(net.parameters(), lr=lr)
     g = torch.Generator(device="cpu").manual_seed(seed)
     for it in range(steps):

@@ -160,3 +160,16 @@ def test_the_plain_hold():
     x[0, :4] = torch.tensor([448.0, 17.0, 2.0 ** -10, 3 * 2.0 ** -10])
     v, byte = R.hold(x, "e4m3", torch.float32)
     assert int(byte[0, 0]) == 127 and v[0, :4].tolist() == [448.0, 16.0, 0.0, 2.0 ** -8]
+
+
+def test_training_layers_need_a_device():
+    import numpy as np
+
+    from paper_2608_15438_amd import train as TR
+    from paper_2608_15438_amd.index_build import Encoder
+    enc = Encoder(weights=[np.eye(4, dtype=np.float32)], biases=[np.zeros(4, np.float32)],
+                  input_scale=1.0)
+    for kw in (dict(layers="hip"), dict(layers="other"), dict(dtype=torch.bfloat16),
+               dict(hold="i8")):
+        with pytest.raises(ValueError):
+            TR._Mlp(enc, "cpu", **kw)
