@@ -7,6 +7,7 @@ or ``__graft_entry__.build()``); importing the binding without it raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import math
 import os
@@ -372,89 +373,98 @@ class Held:
     def device(self):
         return self.q.device
 
+    def get_device(self):
+        return self.q.get_device()
+
     @classmethod
-    def empty(cls, m: int, d: int, fmt: str, dtype, device) -> "Held":
+    def empty(cls, m: int, d: int, fmt: str, like: torch.Tensor) -> "Held":
+        """Room for a matrix [m, d] of the type of `like`, on its device."""
         ldq = (d + 31) // 32 * 32
-        return cls(torch.empty((m, ldq), dtype=_HOLD_DTYPES[fmt], device=device),
-                   torch.empty((m, ldq // 32), dtype=torch.uint8, device=device), d, fmt, dtype)
+        return cls(like.new_empty((m, ldq), dtype=_HOLD_DTYPES[fmt]),
+                   like.new_empty((m, ldq // 32), dtype=torch.uint8), d, fmt, like.dtype)
 
 
-class _On:
-    """The device and stream of a call: outputs and work space are allocated on
-    that stream, so the allocator hands their memory on in its order."""
-
-    def __init__(self, t, stream):
-        self.dev = t.device
-        self.stream = stream
-        self.ctx = None
-
-    def __enter__(self):
-        if self.stream is not None:
-            if self.stream.device != self.dev:
-                raise ValueError(f"the stream is on {self.stream.device}, the tensors on {self.dev}")
-            self.ctx = torch.cuda.stream(self.stream)
-        elif self.dev.index != torch.cuda.current_device():
-            self.ctx = torch.cuda.device(self.dev)
-        if self.ctx is not None:
-            self.ctx.__enter__()
-        return C.c_void_p(torch.cuda.current_stream(self.dev).cuda_stream)
-
-    def __exit__(self, *e):
-        if self.ctx is not None:
-            self.ctx.__exit__(*e)
+_NULL = contextlib.nullcontext()
 
 
-def _mat(t, name, dtype, device, m=None, w=None):
+def _on(t, stream):
+    """Where a call runs: on `stream`, or on the current stream of the tensors'
+    device.  Outputs and work space are allocated on that stream, so the
+    allocator hands their memory on in its order."""
+    if stream is not None:
+        if stream.device != t.device:
+            raise ValueError(f"the stream is on {stream.device}, the tensors on {t.device}")
+        return torch.cuda.stream(stream)
+    if t.get_device() != torch._C._cuda_getDevice():
+        return torch.cuda.device(t.device)
+    return _NULL
+
+
+def _raw(index: int) -> int:
+    """The current stream's handle (what Stream.cuda_stream gives, without the
+    two microseconds that making the object takes)."""
+    return torch._C._cuda_getCurrentRawStream(index)
+
+
+def _mat(t, name, dtype, index, m=None, w=None):
     """(pointer, row stride) of a device matrix whose rows' elements are next to
     each other."""
-    if t.dim() != 2 or (m is not None and t.shape[0] != m) or (w is not None and t.shape[1] != w):
+    s = t.shape
+    if len(s) != 2 or (m is not None and s[0] != m) or (w is not None and s[1] != w):
         raise ValueError(f"{name} must be [{'m' if m is None else m}, {'d' if w is None else w}], "
-                         f"got {list(t.shape)}")
-    if not t.is_cuda or t.dtype != dtype or t.device != device:
-        raise ValueError(f"{name} must be {dtype} on {device}, got {t.dtype} on {t.device}")
-    if t.numel() == 0:
-        return t.data_ptr(), t.shape[1]
-    if t.shape[1] > 1 and t.stride(1) != 1:
+                         f"got {list(s)}")
+    if t.dtype != dtype or t.get_device() != index:
+        raise ValueError(f"{name} must be {dtype} on device {index}, got {t.dtype} on {t.device}")
+    ld, step = t.stride()
+    if step != 1 and s[1] > 1 and s[0] > 0:
         raise ValueError(f"{name}: the elements of a row must be next to each other")
-    ld = t.stride(0)
-    if t.shape[0] > 1 and ld < t.shape[1]:
-        raise ValueError(f"{name}: its rows overlap")
-    return t.data_ptr(), max(ld, t.shape[1]) if t.shape[0] <= 1 else ld
+    if ld < s[1]:
+        if s[0] > 1:
+            raise ValueError(f"{name}: its rows overlap")
+        ld = s[1]
+    return t.data_ptr(), ld
 
 
-def _vec(t, name, dtype, device, n):
+def _vec(t, name, dtype, index, n):
     if t is None:
         return None
-    if tuple(t.shape) != (n,) or not t.is_cuda or t.dtype != dtype or t.device != device:
-        raise ValueError(f"{name} must be {dtype} [{n}] on {device}, "
+    if t.shape != (n,) or t.dtype != dtype or t.get_device() != index:
+        raise ValueError(f"{name} must be {dtype} [{n}] on device {index}, "
                          f"got {t.dtype} {list(t.shape)} on {t.device}")
     if n > 1 and t.stride(0) != 1:
         raise ValueError(f"{name} must be contiguous")
     return t.data_ptr()
 
 
-def _held(h, name, dtype, device, m, d):
+def _held(h, name, dtype, index, m, d):
     """(q pointer, q's row stride, format, scale pointer)"""
     ldq = (d + 31) // 32 * 32
-    if h.fmt not in HOLDS or h.shape != (m, d) or h.dtype != dtype or h.device != device:
-        raise ValueError(f"{name} must hold {dtype} [{m}, {d}] on {device}, got {h.fmt} of "
+    if h.fmt not in HOLDS or h.shape != (m, d) or h.dtype != dtype or h.get_device() != index:
+        raise ValueError(f"{name} must hold {dtype} [{m}, {d}] on device {index}, got {h.fmt} of "
                          f"{h.dtype} {list(h.shape)} on {h.device}")
     _fits(h.q, f"{name}.q", _HOLD_DTYPES[h.fmt], m, ldq)
     _fits(h.scale, f"{name}.scale", torch.uint8, m, ldq // 32)
-    if h.scale.device != device:
-        raise ValueError(f"{name}.scale must be on {device}")
+    if h.scale.get_device() != index:
+        raise ValueError(f"{name}.scale must be on device {index}")
     return h.q.data_ptr(), ldq, HOLDS[h.fmt], h.scale.data_ptr()
 
 
+def _any(t, name, dtype, index, m, w):
+    """(pointer, row stride, format, scale pointer) of a matrix or a held one"""
+    if isinstance(t, Held):
+        return _held(t, name, dtype, index, m, w)
+    return (*_mat(t, name, dtype, index, m, w), 0, None)
+
+
 def _layer_input(t, name):
-    """The input that sets a call's shape, type and device."""
+    """Type and device of the input that sets a call's."""
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
     if t.dtype not in LAYER_DTYPES:
         raise ValueError(f"{name}: {t.dtype} is none of float32, bfloat16 and float16")
     if t.dim() != 2:
         raise ValueError(f"{name} must be a matrix, got {list(t.shape)}")
-    return t.dtype, t.device
+    return t.dtype, t.get_device()
 
 
 def _act(act):
@@ -469,8 +479,15 @@ def _fmt(fmt, name):
     return fmt
 
 
-def _work(nbytes, device):
-    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+def _run(name, desc, like, stream):
+    """One of the calls that take a description and work space."""
+    L = lib()
+    ref = C.byref(desc)
+    n = getattr(L, name + "_ws")(ref)
+    ws = like.new_empty(n, dtype=torch.uint8) if n else None
+    status = getattr(L, name)(ref, None if ws is None else ws.data_ptr(), n, stream)
+    if status != NR_OK:
+        raise NRError(status, name)
 
 
 def nr_act_hold(x: torch.Tensor, fmt: str = "i8", stream=None) -> Held:
@@ -479,10 +496,10 @@ def nr_act_hold(x: torch.Tensor, fmt: str = "i8", stream=None) -> Held:
     _fmt(fmt, "fmt")
     m, d = x.shape
     p, ld = _mat(x, "x", dtype, dev)
-    with _On(x, stream) as s:
-        h = Held.empty(m, d, fmt, dtype, dev)
+    with _on(x, stream):
+        h = Held.empty(m, d, fmt, x)
         _check(lib().nr_act_hold(p, ld, m, d, LAYER_DTYPES[dtype], HOLDS[fmt], h.q.data_ptr(),
-                                 h.scale.data_ptr(), s), "nr_act_hold")
+                                 h.scale.data_ptr(), _raw(dev)), "nr_act_hold")
     return h
 
 
@@ -492,11 +509,12 @@ def nr_act_read(held: Held, dtype=None, stream=None) -> torch.Tensor:
     if dtype not in LAYER_DTYPES:
         raise ValueError(f"{dtype} is none of float32, bfloat16 and float16")
     m, d = held.shape
-    q, ldq, fmt, scale = _held(held, "held", held.dtype, held.device, m, d)
-    with _On(held, stream) as s:
-        y = torch.empty((m, d), dtype=dtype, device=held.device)
-        _check(lib().nr_act_read(q, scale, m, d, fmt, LAYER_DTYPES[dtype], y.data_ptr(), d, s),
-               "nr_act_read")
+    dev = held.get_device()
+    q, ldq, fmt, scale = _held(held, "held", held.dtype, dev, m, d)
+    with _on(held, stream):
+        y = held.q.new_empty((m, d), dtype=dtype)
+        _check(lib().nr_act_read(q, scale, m, d, fmt, LAYER_DTYPES[dtype], y.data_ptr(), d,
+                                 _raw(dev)), "nr_act_read")
     return y
 
 
@@ -506,33 +524,27 @@ def nr_linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = N
     x w^T + bias for the backward pass, pre="i8" or "e4m3" the same in 8 bits."""
     dtype, dev = _layer_input(x, "x")
     m, k = x.shape
-    d = nr_linear_desc()
-    d.x, d.ldx = _mat(x, "x", dtype, dev)
+    xp, ldx = _mat(x, "x", dtype, dev)
     if w.dim() != 2:
         raise ValueError(f"w must be a matrix, got {list(w.shape)}")
     n = w.shape[0]
-    d.w, d.ldw = _mat(w, "w", dtype, dev, n, k)
-    d.m, d.n, d.k, d.dtype, d.act = m, n, k, LAYER_DTYPES[dtype], _act(act)
-    d.bias = _vec(bias, "bias", dtype, dev, n)
-    if residual is not None:
-        d.residual, d.ldr = _mat(residual, "residual", dtype, dev, m, n)
+    wp, ldw = _mat(w, "w", dtype, dev, n, k)
+    bp = _vec(bias, "bias", dtype, dev, n)
+    rp, ldr = (None, 0) if residual is None else _mat(residual, "residual", dtype, dev, m, n)
+    a = _act(act)
     if pre is not True and pre is not False:
         _fmt(pre, "pre")
-    with _On(x, stream) as s:
-        y = torch.empty((m, n), dtype=dtype, device=dev)
-        d.y, d.ldy = y.data_ptr(), n
-        z = None
+    with _on(x, stream):
+        y = x.new_empty((m, n))
+        z, zp, ldz, hold, scale = None, None, 0, 0, None
         if pre is True:
-            z = torch.empty((m, n), dtype=dtype, device=dev)
-            d.pre, d.ldp = z.data_ptr(), n
+            z = x.new_empty((m, n))
+            zp, ldz = z.data_ptr(), n
         elif pre:
-            z = Held.empty(m, n, pre, dtype, dev)
-            d.pre, d.ldp, d.pre_hold, d.pre_scale = (z.q.data_ptr(), z.q.shape[1], HOLDS[pre],
-                                                     z.scale.data_ptr())
-        L = lib()
-        nb = L.nr_linear_ws(C.byref(d))
-        ws = _work(nb, dev)
-        _check(L.nr_linear(C.byref(d), None if ws is None else ws.data_ptr(), nb, s), "nr_linear")
+            z = Held.empty(m, n, pre, x)
+            zp, ldz, hold, scale = z.q.data_ptr(), z.q.shape[1], HOLDS[pre], z.scale.data_ptr()
+        _run("nr_linear", nr_linear_desc(m, n, k, LAYER_DTYPES[dtype], a, xp, ldx, wp, ldw, bp, rp,
+                                         ldr, y.data_ptr(), n, zp, ldz, hold, scale), x, _raw(dev))
     return y if z is None else (y, z)
 
 
@@ -543,41 +555,26 @@ def nr_linear_grad(dy: torch.Tensor, x, w: Optional[torch.Tensor], act: str = "n
     dw, w without dx (but one of the two is needed for their width)."""
     dtype, dev = _layer_input(dy, "dy")
     m, n = dy.shape
-    d = nr_linear_grad_desc()
-    d.dy, d.lddy = _mat(dy, "dy", dtype, dev)
-    d.m, d.n, d.dtype, d.act = m, n, LAYER_DTYPES[dtype], _act(act)
+    dyp, lddy = _mat(dy, "dy", dtype, dev)
+    a = _act(act)
     if (x is None and (dw or w is None)) or (w is None and dx):
         raise ValueError("dw needs x, dx needs w, and one of the two sets the width")
-    k = x.shape[1] if x is not None else w.shape[1]
-    d.k = k
-    if isinstance(x, Held):
-        d.x, d.ldx, d.x_hold, d.x_scale = _held(x, "x", dtype, dev, m, k)
-    elif x is not None:
-        d.x, d.ldx = _mat(x, "x", dtype, dev, m, k)
-    if w is not None:
-        d.w, d.ldw = _mat(w, "w", dtype, dev, n, k)
+    k = x.shape[-1] if x is not None else w.shape[-1]
+    xa = (None, 0, 0, None) if x is None else _any(x, "x", dtype, dev, m, k)
+    wp, ldw = (None, 0) if w is None else _mat(w, "w", dtype, dev, n, k)
+    za = (None, 0, 0, None)
     if act != "none":
         if pre is None:
             raise ValueError(f"act={act!r} needs pre")
-        if isinstance(pre, Held):
-            d.pre, d.ldp, d.pre_hold, d.pre_scale = _held(pre, "pre", dtype, dev, m, n)
-        else:
-            d.pre, d.ldp = _mat(pre, "pre", dtype, dev, m, n)
-    with _On(dy, stream) as s:
-        gx = torch.empty((m, k), dtype=dtype, device=dev) if dx else None
-        gw = torch.empty((n, k), dtype=dtype, device=dev) if dw else None
-        gb = torch.empty(n, dtype=dtype, device=dev) if db else None
-        if dx:
-            d.dx, d.lddx = gx.data_ptr(), k
-        if dw:
-            d.dw, d.lddw = gw.data_ptr(), k
-        if db:
-            d.db = gb.data_ptr()
-        L = lib()
-        nb = L.nr_linear_grad_ws(C.byref(d))
-        ws = _work(nb, dev)
-        _check(L.nr_linear_grad(C.byref(d), None if ws is None else ws.data_ptr(), nb, s),
-               "nr_linear_grad")
+        za = _any(pre, "pre", dtype, dev, m, n)
+    with _on(dy, stream):
+        gx = dy.new_empty((m, k)) if dx else None
+        gw = dy.new_empty((n, k)) if dw else None
+        gb = dy.new_empty(n) if db else None
+        _run("nr_linear_grad",
+             nr_linear_grad_desc(m, n, k, LAYER_DTYPES[dtype], a, dyp, lddy, *xa, wp, ldw, *za,
+                                 gx.data_ptr() if dx else None, k, gw.data_ptr() if dw else None,
+                                 k, gb.data_ptr() if db else None), dy, _raw(dev))
     return gx, gw, gb
 
 
@@ -588,33 +585,32 @@ def nr_layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None,
     what else is asked for: stats (fp32 [2, m]: means and 1 / standard deviations,
     for the backward pass), x and y in 8 bits (hold_x, hold_y: "i8" or "e4m3")."""
     dtype, dev = _layer_input(x, "x")
-    m, w = x.shape
-    d = nr_layer_norm_desc()
-    d.m, d.d, d.dtype, d.eps = m, w, LAYER_DTYPES[dtype], eps
-    d.x, d.ldx = _mat(x, "x", dtype, dev)
-    d.weight = _vec(weight, "weight", dtype, dev, w)
-    d.bias = _vec(bias, "bias", dtype, dev, w)
+    m, d = x.shape
+    xp, ldx = _mat(x, "x", dtype, dev)
+    wp, bp = _vec(weight, "weight", dtype, dev, d), _vec(bias, "bias", dtype, dev, d)
     for f, name in ((hold_x, "hold_x"), (hold_y, "hold_y")):
         if f is not None:
             _fmt(f, name)
-    with _On(x, stream) as s:
-        y = torch.empty((m, w), dtype=dtype, device=dev)
-        d.y, d.ldy = y.data_ptr(), w
+    with _on(x, stream):
+        y = x.new_empty((m, d))
         out = [y]
+        st = None
         if stats:
-            st = torch.empty((2, m), dtype=torch.float32, device=dev)
-            d.stats = st.data_ptr()
+            st = x.new_empty((2, m), dtype=torch.float32)
             out.append(st)
-        if hold_x is not None:
-            h = Held.empty(m, w, hold_x, dtype, dev)
-            d.x_hold, d.xq, d.x_scale = HOLDS[hold_x], h.q.data_ptr(), h.scale.data_ptr()
-            out.append(h)
-        if hold_y is not None:
-            h = Held.empty(m, w, hold_y, dtype, dev)
-            d.y_hold, d.yq, d.y_scale = HOLDS[hold_y], h.q.data_ptr(), h.scale.data_ptr()
-            out.append(h)
-        _check(lib().nr_layer_norm(C.byref(d), s), "nr_layer_norm")
-    return out[0] if len(out) == 1 else tuple(out)
+        held = []
+        for f in (hold_x, hold_y):
+            if f is None:
+                held.append((0, None, None))
+            else:
+                h = Held.empty(m, d, f, x)
+                out.append(h)
+                held.append((HOLDS[f], h.q.data_ptr(), h.scale.data_ptr()))
+        (hx, xq, xs), (hy, yq, ys) = held
+        desc = nr_layer_norm_desc(m, d, LAYER_DTYPES[dtype], eps, xp, ldx, wp, bp, y.data_ptr(), d,
+                                  None if st is None else st.data_ptr(), hx, hy, xq, xs, yq, ys)
+        _check(lib().nr_layer_norm(C.byref(desc), _raw(dev)), "nr_layer_norm")
+    return y if len(out) == 1 else tuple(out)
 
 
 def nr_layer_norm_grad(dy: torch.Tensor, x, stats: torch.Tensor,
@@ -623,36 +619,23 @@ def nr_layer_norm_grad(dy: torch.Tensor, x, stats: torch.Tensor,
     """(dx, dweight, dbias) of nr_layer_norm, None for those not asked for; `add`
     (the gradient that reaches x on another path) is added to dx.  x may be Held."""
     dtype, dev = _layer_input(dy, "dy")
-    m, w = dy.shape
-    d = nr_layer_norm_grad_desc()
-    d.m, d.d, d.dtype = m, w, LAYER_DTYPES[dtype]
-    d.dy, d.lddy = _mat(dy, "dy", dtype, dev)
-    if isinstance(x, Held):
-        d.x, d.ldx, d.x_hold, d.x_scale = _held(x, "x", dtype, dev, m, w)
-    else:
-        d.x, d.ldx = _mat(x, "x", dtype, dev, m, w)
+    m, d = dy.shape
+    dyp, lddy = _mat(dy, "dy", dtype, dev)
+    xa = _any(x, "x", dtype, dev, m, d)
     _fits(stats, "stats", torch.float32, 2, m)
-    if stats.device != dev:
-        raise ValueError(f"stats must be on {dev}")
-    d.stats = stats.data_ptr()
-    d.weight = _vec(weight, "weight", dtype, dev, w)
-    if add is not None:
-        d.add, d.ldadd = _mat(add, "add", dtype, dev, m, w)
-    with _On(dy, stream) as s:
-        gx = torch.empty((m, w), dtype=dtype, device=dev) if dx else None
-        gw = torch.empty(w, dtype=dtype, device=dev) if dweight else None
-        gb = torch.empty(w, dtype=dtype, device=dev) if dbias else None
-        if dx:
-            d.dx, d.lddx = gx.data_ptr(), w
-        if dweight:
-            d.dweight = gw.data_ptr()
-        if dbias:
-            d.dbias = gb.data_ptr()
-        L = lib()
-        nb = L.nr_layer_norm_grad_ws(C.byref(d))
-        ws = _work(nb, dev)
-        _check(L.nr_layer_norm_grad(C.byref(d), None if ws is None else ws.data_ptr(), nb, s),
-               "nr_layer_norm_grad")
+    if stats.get_device() != dev:
+        raise ValueError(f"stats must be on device {dev}")
+    wp = _vec(weight, "weight", dtype, dev, d)
+    ap, lda = (None, 0) if add is None else _mat(add, "add", dtype, dev, m, d)
+    with _on(dy, stream):
+        gx = dy.new_empty((m, d)) if dx else None
+        gw = dy.new_empty(d) if dweight else None
+        gb = dy.new_empty(d) if dbias else None
+        _run("nr_layer_norm_grad",
+             nr_layer_norm_grad_desc(m, d, LAYER_DTYPES[dtype], dyp, lddy, *xa, stats.data_ptr(),
+                                     wp, ap, lda, gx.data_ptr() if dx else None, d,
+                                     gw.data_ptr() if dweight else None,
+                                     gb.data_ptr() if dbias else None), dy, _raw(dev))
     return gx, gw, gb
 
 
