@@ -9,6 +9,7 @@
 // neighbouring elements of a row of the output.  Where the tiles are few and k
 // long, k is cut and the parts' fp32 sums are added in order by a second kernel
 // with the same epilogue.
+#include <cmath>
 #include <type_traits>
 
 #include "nr_layers.h"
@@ -18,9 +19,11 @@ namespace nr {
 typedef float v4f __attribute__((ext_vector_type(4)));
 
 struct GemmArgs {
-  int64_t I, K, kchunk;  // k of a part, a multiple of the K-tile
+  int64_t I, K, kchunk;  // k of a part, a multiple of the K-tiles
   int J;
   LayerMat A, B;         // B may be held in 8 bits where j runs along its rows
+  int64_t grid;          // blocks per part
+  int parts;
   float *part;           // [parts][I][ldp] sums of the parts, or NULL
   int64_t ldp;
   void *out;             // without the layer's epilogue: [I][ldo]
@@ -125,19 +128,52 @@ struct Operand {
   // where chunk c of a row lies, and (the exchange being its own inverse) the
   // chunk that lies at place c
   static __device__ __forceinline__ int swap(int row, int c) {
-    if constexpr (KC && BK == 64) return c ^ (row & 7);
+    if constexpr (KC && BK == 128) return c ^ (row & 15);
+    else if constexpr (KC && BK == 64) return c ^ (row & 7);
     else if constexpr (KC) return c ^ ((row >> 3) & 1) << 1;
     else if constexpr (R >= 128) return c ^ (((row & 3) | ((row >> 3) & 1) << 2) << 1);
     else return c ^ ((row & 3) << 1);
   }
   static __device__ __forceinline__ int slot(int row, int c) { return row * CPR + swap(row, c); }
 
-  // [o0, o0 + R) x [k, k + BK).  Past kend, and past nO where the side runs along
-  // the rows, zeros; rows of a KC operand past nO repeat the last (their outputs
-  // are dropped).  FULL: nothing is past an end
+  // eight elements from p on as they are in memory, at any alignment of the
+  // element; of a chunk that reaches past the row's end at n, zeros from there
+  // on.  room: elements from p to the matrix's last, beyond which nothing is read
+  static __device__ __forceinline__ void load(uint4 (&o)[sizeof(T) / 2], const T *p, int n,
+                                              int64_t room) {
+    constexpr int W = 2 * sizeof(T);   // words of a chunk
+    uint32_t v[W];
+    if (room >= 8) {
+      __builtin_memcpy(v, p, sizeof v);
+    } else {   // the last chunk of the last row
+#pragma unroll
+      for (int w = 0; w < W; ++w) v[w] = 0;
+#pragma unroll 1
+      for (int i = 0; i < n; ++i) {
+        uint32_t x = 0;
+        __builtin_memcpy(&x, p + i, sizeof(T));
+        x <<= sizeof(T) == 2 ? 16 * (i & 1) : 0;
+        const int at = sizeof(T) == 2 ? i >> 1 : i;
+#pragma unroll
+        for (int w = 0; w < W; ++w) v[w] |= w == at ? x : 0;
+      }
+    }
+    if (n < 8)
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        if (sizeof(T) == 2) v[w] = 2 * w + 1 < n ? v[w] : 2 * w < n ? v[w] & 0xffffu : 0;
+        else v[w] = w < n ? v[w] : 0;
+      }
+    __builtin_memcpy(o, v, sizeof v);
+  }
+
+  // [o0, o0 + R) x [k, k + BK) of a matrix whose rows have `width` elements.  Past
+  // kend, and past nO where the side runs along the rows, zeros; rows of a KC
+  // operand past nO repeat the last (their outputs are dropped).  FULL: nothing is
+  // past an end
   template <bool FULL>
   __device__ __forceinline__ void fetch(const LayerMat &m, int64_t o0, int64_t nO, int64_t k,
-                                        int64_t kend) {
+                                        int64_t kend, int64_t K) {
 #pragma unroll
     for (int u = 0; u < N; ++u) {
       const int e = threadIdx.x + NT * u;
@@ -153,15 +189,14 @@ struct Operand {
           q[u] = *reinterpret_cast<const uint2 *>((const uint8_t *)m.p + row * m.ld + col);
           scale[u] = m.scale[row * (m.ld / 32) + col / 32];
         }
+      } else if constexpr (FULL) {
+        __builtin_memcpy(raw[u], (const T *)m.p + row * m.ld + col, 8 * sizeof(T));
       } else {
-        const T *p = (const T *)m.p + row * m.ld + col;
-        if (FULL || (in && col + 8 <= cols)) {
-          __builtin_memcpy(raw[u], p, 8 * sizeof(T));   // any alignment of the element
-        } else {
-          T v[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = in && col + i < cols ? p[i] : (T)0.0f;
-          __builtin_memcpy(raw[u], v, 8 * sizeof(T));
+        __builtin_memset(raw[u], 0, 8 * sizeof(T));
+        if (in && col < cols) {
+          const int64_t at = row * m.ld + col;
+          load(raw[u], (const T *)m.p + at, cols - col < 8 ? (int)(cols - col) : 8,
+               ((KC ? nO : K) - 1) * m.ld + (KC ? K : nO) - at);
         }
       }
     }
@@ -210,7 +245,7 @@ struct Operand {
       const int e = threadIdx.x + NT * u;
       int row = e / CPR, c = swap(row, e % CPR);
       if (KC) row = row < left ? row : (int)left - 1;
-      else c = 8 * c < left ? c : (int)(left / 8) - 1;
+      else c = 8 * c < left ? c : (int)((left - 1) / 8);
       offset[u] = (uint32_t)(row * m.ld + 8 * c) * (uint32_t)sizeof(T);
     }
   }
@@ -285,7 +320,8 @@ __device__ float plain_chain(const LayerMat &A, const LayerMat &B, int64_t i, in
 // floats are exchanged by the row's number against bank conflicts
 template <class T, int NI, int NJ, bool IK, bool JK, bool HELD, bool LIN>
 __device__ __forceinline__ void write_tile(const GemmArgs &a, const v4f (&acc)[NI][NJ], char *lds,
-                                           int64_t i0, int64_t j0, int64_t k0, int64_t k1) {
+                                           int64_t i0, int64_t j0, int part, int64_t k0,
+                                           int64_t k1) {
   constexpr int W = 16 * NJ, CH = W / 4, LPR = W / 8;    // columns, chunks and lanes of a row
   constexpr int RPS = WAVE / LPR, NS = 16 / RPS;         // rows per step, steps
   const int lane = threadIdx.x & (WAVE - 1), c = 2 * (lane % LPR);
@@ -339,7 +375,7 @@ __device__ __forceinline__ void write_tile(const GemmArgs &a, const v4f (&acc)[N
       }
       if (a.part) {
         if (i < a.I && j < a.ldp) {
-          float4 *o = reinterpret_cast<float4 *>(a.part + ((int64_t)blockIdx.y * a.I + i) * a.ldp + j);
+          float4 *o = reinterpret_cast<float4 *>(a.part + ((int64_t)part * a.I + i) * a.ldp + j);
           o[0] = make_float4(v[0], v[1], v[2], v[3]);
           o[1] = make_float4(v[4], v[5], v[6], v[7]);
         }
@@ -390,20 +426,27 @@ __device__ __forceinline__ void multiply(const char *la, const char *lb, int wi,
 // blocks of 16 x 16.  The next K-tile is read into registers while this one is
 // multiplied.  Blocks go to the eight XCDs in turn: each XCD takes a run of
 // neighbouring tiles, so that their operands meet in its L2.
-template <class T, int TI, int TJ, bool IK, bool JK, bool HELD, bool LIN>
-__global__ void __launch_bounds__(256, 2) k_gemm(GemmArgs a) {
-  typedef Operand<T, TI, IK, false> OA;
-  typedef Operand<T, TJ, JK, HELD> OB;
-  constexpr int BK = OA::BK, NBUF = Tile<T>::NBUF;
-  constexpr int NI = TI / 32, NJ = TJ / 32;
-  __shared__ __attribute__((aligned(16))) char lds[NBUF][OA::BYTES + OB::BYTES];
+// Tiles of 64 x 64 take K-tiles twice as long: what they lack is loads under way.
+template <class T, int S>
+struct RegTile {
+  static constexpr int BK = S == 64 ? 2 * Tile<T>::BK : Tile<T>::BK;
+  static constexpr int NBUF = S == 64 ? 1 : Tile<T>::NBUF;
+  static constexpr int BYTES = NBUF * Tile<T>::P * 2 * S * BK * 2;
+};
+template <class T, int S, bool IK, bool JK, bool HELD, bool LIN>
+__device__ __forceinline__ void gemm_body(const GemmArgs &a, char *lds, int64_t block) {
+  constexpr int TI = S, TJ = S, BK = RegTile<T, S>::BK, NBUF = RegTile<T, S>::NBUF;
+  typedef Operand<T, TI, IK, false, 256, BK> OA;
+  typedef Operand<T, TJ, JK, HELD, 256, BK> OB;
+  constexpr int NI = TI / 32, NJ = TJ / 32, BUF = OA::BYTES + OB::BYTES;
   const int lane = lane_id(), wave = threadIdx.x / WAVE;
   const int wi = TI / 2 * (wave & 1), wj = TJ / 2 * (wave >> 1);
   const int64_t ti = (a.I + TI - 1) / TI, tj = (a.J + TJ - 1) / TJ, tiles = ti * tj;
   const int64_t per = (tiles + 7) / 8;
-  const int64_t k0 = (int64_t)blockIdx.y * a.kchunk;
+  const int part = (int)(block / a.grid);
+  const int64_t k0 = part * a.kchunk;
   const int64_t k1 = k0 + a.kchunk < a.K ? k0 + a.kchunk : a.K;
-  for (int64_t u = blockIdx.x; u < 8 * per; u += gridDim.x) {
+  for (int64_t u = block - part * a.grid; u < 8 * per; u += a.grid) {
     const int64_t t = (u & 7) * per + (u >> 3);
     if (t >= tiles) continue;   // the whole block together
     int64_t i0, j0;
@@ -414,16 +457,16 @@ __global__ void __launch_bounds__(256, 2) k_gemm(GemmArgs a) {
     OB fb;
     auto fetch = [&](int64_t k) {
       if (inside && k + BK <= k1) {
-        fa.template fetch<true>(a.A, i0, a.I, k, k1);
-        fb.template fetch<true>(a.B, j0, a.J, k, k1);
+        fa.template fetch<true>(a.A, i0, a.I, k, k1, a.K);
+        fb.template fetch<true>(a.B, j0, a.J, k, k1, a.K);
       } else {
-        fa.template fetch<false>(a.A, i0, a.I, k, k1);
-        fb.template fetch<false>(a.B, j0, a.J, k, k1);
+        fa.template fetch<false>(a.A, i0, a.I, k, k1, a.K);
+        fb.template fetch<false>(a.B, j0, a.J, k, k1, a.K);
       }
     };
     auto stash = [&](int buf) {
-      fa.stash(lds[buf], 0);
-      fb.stash(lds[buf] + OA::BYTES, a.B.hold);
+      fa.stash(lds + buf * BUF, 0);
+      fb.stash(lds + buf * BUF + OA::BYTES, a.B.hold);
     };
     v4f acc[NI][NJ];
 #pragma unroll
@@ -440,7 +483,7 @@ __global__ void __launch_bounds__(256, 2) k_gemm(GemmArgs a) {
     for (int64_t k = k0; k < k1; k += BK) {
       const bool more = k + BK < k1;
       if (more) fetch(k + BK);
-      multiply<OA, OB>(lds[buf], lds[buf] + OA::BYTES, wi, wj, acc);
+      multiply<OA, OB>(lds + buf * BUF, lds + buf * BUF + OA::BYTES, wi, wj, acc);
       if (NBUF == 1) __syncthreads();
       if (more) {
         if (NBUF == 2) buf ^= 1;
@@ -449,9 +492,24 @@ __global__ void __launch_bounds__(256, 2) k_gemm(GemmArgs a) {
       }
     }
     __syncthreads();   // the last K-tile has been read
-    write_tile<T, NI, NJ, IK, JK, HELD, LIN>(a, acc, (char *)lds + wave * 1024 * NJ, i0 + wi,
-                                             j0 + wj, k0, k1);
+    write_tile<T, NI, NJ, IK, JK, HELD, LIN>(a, acc, lds + wave * 1024 * NJ, i0 + wi, j0 + wj,
+                                             part, k0, k1);
   }
+}
+
+template <class T, int S, bool IK, bool JK, bool HELD, bool LIN>
+__global__ void __launch_bounds__(256, 2) k_gemm(GemmArgs a) {
+  __shared__ __attribute__((aligned(16))) char lds[RegTile<T, S>::BYTES];
+  gemm_body<T, S, IK, JK, HELD, LIN>(a, lds, blockIdx.x);
+}
+
+// dx and dw in one launch, where both take small tiles
+template <class T, bool HELD>
+__global__ void __launch_bounds__(256, 2) k_gemm_two(GemmArgs x, GemmArgs w) {
+  __shared__ __attribute__((aligned(16))) char lds[RegTile<T, 64>::BYTES];
+  const int64_t nw = w.grid * w.parts;
+  if (blockIdx.x < nw) gemm_body<T, 64, false, false, HELD, false>(w, lds, blockIdx.x);
+  else gemm_body<T, 64, true, false, false, false>(x, lds, blockIdx.x - nw);
 }
 
 // The same for 16-bit operands whose rows lie on 16-byte boundaries: K-tiles go
@@ -471,7 +529,8 @@ __global__ void __launch_bounds__(256, 2) k_gemm_dma(GemmArgs a) {
   const int wi = TI / 2 * (wave & 1), wj = TJ / 2 * (wave >> 1);
   const int64_t ti = (a.I + TI - 1) / TI, tj = (a.J + TJ - 1) / TJ, tiles = ti * tj;
   const int64_t per = (tiles + 7) / 8;
-  const int64_t k0 = (int64_t)blockIdx.y * a.kchunk;
+  const int part = (int)(blockIdx.x / a.grid);
+  const int64_t k0 = part * a.kchunk;
   const int64_t k1 = k0 + a.kchunk < a.K ? k0 + a.kchunk : a.K;
   int in = 0, out = 0;          // LDS buffers to fill and to read next
   int64_t i0 = 0, j0 = 0, left = 0;   // the tile; k of it not yet asked for
@@ -494,7 +553,7 @@ __global__ void __launch_bounds__(256, 2) k_gemm_dma(GemmArgs a) {
   // the block's next tile from its u-th on (-1: none left), its first two K-tiles
   // asked for
   auto begin = [&](int64_t u) -> int64_t {
-    for (; u < 8 * per; u += gridDim.x)
+    for (; u < 8 * per; u += a.grid)
       if ((u & 7) * per + (u >> 3) < tiles) {
         tile_at((u & 7) * per + (u >> 3), ti, tj, i0, j0);
         i0 *= TI, j0 *= TJ;
@@ -519,7 +578,7 @@ __global__ void __launch_bounds__(256, 2) k_gemm_dma(GemmArgs a) {
   std::integral_constant<int, 0> ALL;
   std::integral_constant<int, OA::N + OB::N> BUT_LAST;
   const int64_t nk = (k1 - k0 + BK - 1) / BK;
-  int64_t u = begin(blockIdx.x);
+  int64_t u = begin(blockIdx.x - part * a.grid);
   while (u >= 0) {
     v4f acc[NI][NJ];
 #pragma unroll
@@ -554,18 +613,18 @@ __global__ void __launch_bounds__(256, 2) k_gemm_dma(GemmArgs a) {
     // the next tile's first K-tiles come while this one is finished; the third
     // buffer is free for that
     const int64_t i1 = i0 + wi, j1 = j0 + wj;
-    u = begin(u + gridDim.x);
-    write_tile<T, NI, NJ, IK, JK, false, LIN>(a, acc, lds + in + wave * 1024 * NJ, i1, j1, k0, k1);
+    u = begin(u + a.grid);
+    write_tile<T, NI, NJ, IK, JK, false, LIN>(a, acc, lds + in + wave * 1024 * NJ, i1, j1, part,
+                                              k0, k1);
     __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): nothing is under way into registers
   }
 }
 
 // The parts' sums, in order, and the epilogue: eight columns of a row per thread
 template <class T, bool LIN>
-__global__ void __launch_bounds__(256) k_gemm_join(GemmArgs a, int parts) {
+__device__ __forceinline__ void join_body(const GemmArgs &a, int64_t block, int64_t blocks) {
   const int64_t per = a.ldp / 8, units = a.I * per;   // whole quads per row
-  for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < units;
-       u += (int64_t)gridDim.x * 256) {
+  for (int64_t u = block * 256 + threadIdx.x; u < units; u += blocks * 256) {
     const int64_t i = u / per;
     const int j = (int)(u - i * per) * 8;
     float v[8] = {};
@@ -574,7 +633,8 @@ __global__ void __launch_bounds__(256) k_gemm_join(GemmArgs a, int parts) {
       if (a.lin.bias) bias.load((const T *)a.lin.bias, j, a.J);
       if (a.lin.res) res.load((const T *)a.lin.res + i * a.lin.ldr, j, a.J);
     }
-    for (int s = 0; s < parts; ++s) {
+#pragma unroll 4
+    for (int s = 0; s < a.parts; ++s) {
       const float4 *p =
           reinterpret_cast<const float4 *>(a.part + ((int64_t)s * a.I + i) * a.ldp + j);
       const float4 x = p[0], y = p[1];
@@ -585,8 +645,56 @@ __global__ void __launch_bounds__(256) k_gemm_join(GemmArgs a, int parts) {
   }
 }
 
-// dz = dy act'(pre) of `rows` rows per block, rounded to the type (dz NULL: not
-// wanted), and its column sums over them (part NULL: not wanted).  The 256
+template <class T>
+__global__ void __launch_bounds__(256) k_linear_join(GemmArgs a) {
+  join_body<T, true>(a, blockIdx.x, gridDim.x);
+}
+
+// rows of d elements with a stride of ld, as rows with a stride of ldo (a multiple
+// of 8), zeros behind d
+template <class T>
+__global__ void __launch_bounds__(256) k_pad_rows(const T *x, int64_t ld, int64_t m, int d, T *out,
+                                                  int64_t ldo) {
+  const int64_t per = ldo / 8, units = m * per;
+  for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < units;
+       u += (int64_t)gridDim.x * 256) {
+    const int64_t r = u / per;
+    const int c = (int)(u - r * per) * 8;
+    Raw8<T> v;
+    v.load(x + r * ld, c, d);
+    *reinterpret_cast<typename Raw8<T>::t8 *>(out + r * ldo + c) = v.v;
+  }
+}
+
+// What is left of the gradients: bx blocks join dx, bw join dw, the others add up
+// the column sums of dz, sixteen columns each (sixteen threads of a column add
+// every sixteenth row, then the sixteen sums in order)
+template <class T>
+__global__ void __launch_bounds__(256) k_grad_join(GemmArgs x, GemmArgs w, int64_t bx, int64_t bw,
+                                                   const float *cols, int64_t rows, int n, T *db) {
+  __shared__ float red[16][17];
+  int64_t b = blockIdx.x;
+  if (b < bx) return join_body<T, false>(x, b, bx);
+  b -= bx;
+  if (b < bw) return join_body<T, false>(w, b, bw);
+  b -= bw;
+  const int c = (int)b * 16 + (threadIdx.x & 15), q = threadIdx.x >> 4;
+  float v = 0.0f;
+  if (c < n) {
+#pragma unroll 8
+    for (int64_t r = q; r < rows; r += 16) v += cols[r * n + c];
+  }
+  red[q][threadIdx.x & 15] = v;
+  __syncthreads();
+  if (q == 0 && c < n) {
+#pragma unroll
+    for (int i = 1; i < 16; ++i) v += red[i][threadIdx.x];
+    db[c] = from_f32<T>(v);
+  }
+}
+
+// dz = dy act'(pre) of `rows` rows per block, rounded to the type, zeros from n up to
+// ldz (a multiple of 32; dz NULL: not wanted), and its column sums over them (part NULL: not wanted).  The 256
 // threads are 256 / ct rows of ct threads, eight columns each
 template <class T>
 __global__ void __launch_bounds__(256) k_act_grad(LinearGradArgs a, int64_t rows, int ct, T *dz,
@@ -597,12 +705,12 @@ __global__ void __launch_bounds__(256) k_act_grad(LinearGradArgs a, int64_t rows
   const int c0 = (blockIdx.y * ct + tc) * 8;
   const int64_t r0 = (int64_t)blockIdx.x * rows, r1 = r0 + rows < a.m ? r0 + rows : a.m;
   float s[8] = {};
-  if (c0 < a.n)
+  if (c0 < ldz)
     for (int64_t r = r0 + tr; r < r1; r += rt) {
       float v[8], z[8];
       load8((const T *)a.dy + r * a.lddy, c0, a.n, v);
       if (a.act != NR_ACT_NONE) {
-        if (a.pre.hold)
+        if (a.pre.hold)   // (its rows are padded as dz's are)
           read8<T>((const uint8_t *)a.pre.p + r * a.pre.ld, a.pre.scale + r * (a.pre.ld / 32), c0,
                 a.pre.hold, z);
         else
@@ -610,9 +718,12 @@ __global__ void __launch_bounds__(256) k_act_grad(LinearGradArgs a, int64_t rows
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] *= act_slope<exact>(z[i], a.act);
       }
-      if (dz) store8(dz + r * ldz, c0, a.n, v);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s[i] += c0 + i < a.n ? v[i] : 0.0f;
+      for (int i = 0; i < 8; ++i) {
+        v[i] = c0 + i < a.n ? v[i] : 0.0f;   // (a slope of what is behind the width)
+        s[i] += v[i];
+      }
+      if (dz) store8(dz + r * ldz, c0, (int)ldz, v);
     }
   if (!part) return;
 #pragma unroll
@@ -635,29 +746,65 @@ static bool aligned(const void *p, int64_t ld, size_t e, size_t to) {
   return !p || (reinterpret_cast<uintptr_t>(p) % to == 0 && ld * e % to == 0);
 }
 
-// How a product is cut: the tile's side, and parts of k.  Larger tiles read less
-// of LDS and memory for an output, if there are enough of them to go round
+// How a product is cut: the tile's side (256: 256 x 128), and parts of k.  The
+// cheapest by this estimate of its time in us, from rates measured on MI355X:
+// a block's share of a CU that is kept busy by two goes at `rate` / 256
+// (TFLOP/s, by tile; products with both operands transposed less in small
+// tiles), one alone on its CU at 4/5 of that; parts cost a launch and their sums
+// pass through memory (the last-level cache) twice at 10 TB/s.  Estimate /
+// measured: 10,000 x 1536 -> 512 fp32 in 64 x 64 121 / 115, 128 x 128 140 / 118, in
+// four parts 114 / 109; 4096 x 1024 -> 256 bf16 64 x 64 12 / 12, 128 x 128 18 / 18;
+// 16,384 x 512 -> 512 bf16 27 / 27, 26 / 19, 256 x 128 32 / 27; dw of 4096 rows, 1024 x
+// 256, bf16 64 x 64 in four parts 19 / 23, 128 x 128 in eight 17 / 18
 struct Split {
   int side, parts;
   int64_t kchunk;
 };
-static Split split_of(int64_t I, int J, int64_t K, int dtype) {
-  auto tiles = [&](int64_t t) { return up(I, t) / t * (up(J, t) / t); };
-  Split sp{128, 1, 64};
-  if (dtype != NR_F32 && tiles(256) >= 256) sp.side = 256;   // 256 x 128
-  else if (tiles(128) < 256 && tiles(128) * (K / 512) < 256) sp.side = 64;
-  const int64_t n = tiles(sp.side);
-  int64_t parts = n > 0 && n < 256 ? (512 + n - 1) / n : 1;
-  const int64_t most = K / 256 < 64 ? K / 256 : 64;
-  if (parts > most) parts = most;
-  if (parts < 2) parts = 1;
-  sp.kchunk = K > 0 ? up((K + parts - 1) / parts, 64) : 64;
-  sp.parts = K > 0 ? (int)((K + sp.kchunk - 1) / sp.kchunk) : 1;
-  return sp;
+static Split split_of(int64_t I, int J, int64_t K, int dtype, bool both_transposed) {
+  struct Kind {
+    int side, ti, tj;
+    double rate;
+  };
+  const bool f32 = dtype == NR_F32;
+  const Kind kinds[3] = {{64, 64, 64, f32 ? 145.0 : both_transposed ? 280.0 : 390.0},
+                         {128, 128, 128, f32 ? 190.0 : 800.0},
+                         {256, 256, 128, 950.0}};
+  Split best{64, 1, 128};
+  double least = 0.0;
+  for (int q = 0; q < (f32 ? 2 : 3); ++q) {
+    const Kind &kind = kinds[q];
+    const double tiles = (double)(up(I, kind.ti) / kind.ti) * (double)(up(J, kind.tj) / kind.tj);
+    for (int want = 1; want <= 64; want *= 2) {
+      if (want > 1 && (K < 256 * want || tiles * want > 2048)) break;
+      const int64_t kc = K > 0 ? up((K + want - 1) / want, 128) : 128;
+      const int parts = K > 0 ? (int)((K + kc - 1) / kc) : 1;
+      const double block = 2e-6 * kind.ti * kind.tj * kc / (kind.rate / 256);
+      const double per_cu = std::ceil(tiles * parts / 256);
+      const double us = block * (per_cu + (std::fmod(per_cu, 2.0) == 1.0 ? 0.25 : 0.0)) +
+                        (parts > 1 ? 4.0 + 8e-7 * parts * (double)I * J : 0.0);
+      if ((q == 0 && want == 1) || us < least) {
+        least = us;
+        best = Split{kind.side, parts, kc};
+      }
+    }
+  }
+#ifdef NR_EXPERIMENT
+  int64_t parts = best.parts;
+  if (const char *f = getenv("NR_SIDE")) best.side = atoi(f);
+  if (const char *f = getenv("NR_PARTS")) {
+    parts = atoi(f);
+    const int64_t most = K / 256 < 64 ? K / 256 : 64;
+    if (parts > most) parts = most;
+    if (parts < 2) parts = 1;
+    best.kchunk = K > 0 ? up((K + parts - 1) / parts, 128) : 128;
+    best.parts = K > 0 ? (int)((K + best.kchunk - 1) / best.kchunk) : 1;
+  }
+#endif
+  return best;
 }
-static size_t part_bytes(int64_t I, int J, int64_t K, int dtype) {
-  const Split sp = split_of(I, J, K, dtype);
-  return sp.parts > 1 ? sizeof(float) * (size_t)sp.parts * I * up(J, 32) : 0;
+static size_t part_bytes(int64_t I, int J, int64_t K, int dtype, bool both_transposed) {
+  const Split sp = split_of(I, J, K, dtype, both_transposed);
+  return sp.parts > 1 ? up(sizeof(float) * (size_t)sp.parts * I * up(J, 32), 256) : 0;
 }
 
 template <class T>
@@ -665,101 +812,176 @@ static constexpr int type_of() {
   return sizeof(T) == 4 ? NR_F32 : __is_same(T, bf16_t) ? NR_BF16 : NR_F16;
 }
 
-// an operand that can go straight into LDS: whole chunks in rows on 16-byte
-// boundaries, a tile of them within 2^32 bytes
+// an operand that can go straight into LDS: whole chunks (or zeros up to the row
+// stride) in rows on 16-byte boundaries, a tile of them within 2^32 bytes
 static bool direct(const LayerMat &m, int64_t width) {
-  return !m.hold && aligned(m.p, m.ld, 2, 16) && m.ld < (int64_t)1 << 22 && width % 8 == 0;
+  return !m.hold && aligned(m.p, m.ld, 2, 16) && m.ld < (int64_t)1 << 22 &&
+         (width % 8 == 0 || m.padded);
+}
+
+// Rows that lie off the 16-byte boundaries can be read, but not straight into LDS,
+// and a load across two lines costs two: us of bf16 products at widths of 1024 /
+// 1023, 16,384 rows: y 50 / 73, dx 38 / 94, dw 61 / 111.  A copy with padded rows
+// (k_pad_rows, 4 bytes of traffic an element at some 5 TB/s and a launch) pays
+// where an element goes into enough products: `products` per element of it
+static bool copy_pays(int dtype, int64_t rows, int64_t width, int64_t ld, int64_t products,
+                      int side, int64_t from) {
+  return dtype != NR_F32 && side >= 128 && (width % 8 != 0 || ld % 8 != 0) && rows > 0 &&
+         products >= from;
+}
+
+static int64_t tile_grid(const GemmArgs &a, int ti, int tj) {
+  const int64_t n = up(up(a.I, ti) / ti * (up(a.J, tj) / tj), 8);
+  return n < 1 << 20 ? n : 1 << 20;   // blocks take further tiles in turn
+}
+
+// a product's parts and their place; returns the tile's side
+template <class T>
+static int place(GemmArgs &a, float *ws, bool both_transposed) {
+  const Split sp = split_of(a.I, a.J, a.K, type_of<T>(), both_transposed);
+  a.kchunk = sp.kchunk;
+  a.parts = sp.parts;
+  a.part = sp.parts > 1 ? ws : nullptr;
+  a.ldp = up(a.J, 32);
+  return sp.side;
+}
+static int64_t join_blocks(const GemmArgs &a) {
+  if (a.parts < 2) return 0;
+  const int64_t b = (a.I * (a.ldp / 8) + 255) / 256;
+  return b < 1 << 20 ? b : 1 << 20;
 }
 
 template <class T, int S, bool IK, bool JK, bool LIN>
-static void gemm_tiles(const GemmArgs &a, int parts, hipStream_t s) {
-  const int64_t tiles = up(up(a.I, S) / S * (up(a.J, S) / S), 8);
-  const dim3 g((unsigned)(tiles < 1 << 22 ? tiles : 1 << 22), parts);
-  if constexpr (sizeof(T) == 2 && S >= 128) {
-    if (direct(a.A, IK ? a.K : a.I) && direct(a.B, JK ? a.K : a.J)) {
-      const int64_t n = up(up(a.I, S) / S * (up(a.J, 128) / 128), 8);
-      const int64_t room = up(512 / parts > 0 ? 512 / parts : 1, 8);   // two blocks a CU
-      hipLaunchKernelGGL((k_gemm_dma<T, S, 128, IK, JK, LIN>),
-                         dim3((unsigned)(n < room ? n : room), parts), dim3(256), 0, s, a);
+static void gemm_reg(GemmArgs &a, hipStream_t s) {
+  a.grid = tile_grid(a, S, S);
+  const dim3 g((unsigned)(a.grid * a.parts));
+  if constexpr (!IK) {
+    if (a.B.hold) {
+      hipLaunchKernelGGL((k_gemm<T, S, IK, JK, true, LIN>), g, dim3(256), 0, s, a);
       return;
     }
   }
-  if constexpr (S < 256) {
-    if constexpr (!IK) {
-      if (a.B.hold) {
-        hipLaunchKernelGGL((k_gemm<T, S, S, IK, JK, true, LIN>), g, dim3(256), 0, s, a);
-        return;
-      }
-    }
-    hipLaunchKernelGGL((k_gemm<T, S, S, IK, JK, false, LIN>), g, dim3(256), 0, s, a);
-  } else {
-    gemm_tiles<T, 128, IK, JK, LIN>(a, parts, s);
-  }
+  hipLaunchKernelGGL((k_gemm<T, S, IK, JK, false, LIN>), g, dim3(256), 0, s, a);
 }
 
 template <class T, bool IK, bool JK, bool LIN>
-static hipError_t gemm(GemmArgs a, float *ws, hipStream_t s) {
-  if (a.I <= 0) return hipSuccess;
-  const Split sp = split_of(a.I, a.J, a.K, type_of<T>());
-  a.kchunk = sp.kchunk;
-  a.part = sp.parts > 1 ? ws : nullptr;
-  a.ldp = up(a.J, 32);
-  if (sp.side == 64) gemm_tiles<T, 64, IK, JK, LIN>(a, sp.parts, s);
-  else if (sizeof(T) == 4 || sp.side == 128) gemm_tiles<T, 128, IK, JK, LIN>(a, sp.parts, s);
-  else if constexpr (sizeof(T) == 2) gemm_tiles<T, 256, IK, JK, LIN>(a, sp.parts, s);
-  if (sp.parts > 1) {
-    const int64_t blocks = (a.I * (a.ldp / 8) + 255) / 256;
-    hipLaunchKernelGGL((k_gemm_join<T, LIN>), dim3((unsigned)(blocks < 1 << 20 ? blocks : 1 << 20)),
-                       dim3(256), 0, s, a, sp.parts);
+static void gemm(GemmArgs &a, int side, hipStream_t s) {
+  if (a.I <= 0) return;
+  if constexpr (sizeof(T) == 2) {
+    if (side >= 128 && direct(a.A, IK ? a.K : a.I) && direct(a.B, JK ? a.K : a.J)) {
+      const int64_t room = up(512 / a.parts > 0 ? 512 / a.parts : 1, 8);   // two blocks a CU
+      const int64_t n = tile_grid(a, side, 128);
+      a.grid = n < room ? n : room;
+      const dim3 g((unsigned)(a.grid * a.parts));
+      if (side == 256)
+        hipLaunchKernelGGL((k_gemm_dma<T, 256, 128, IK, JK, LIN>), g, dim3(256), 0, s, a);
+      else
+        hipLaunchKernelGGL((k_gemm_dma<T, 128, 128, IK, JK, LIN>), g, dim3(256), 0, s, a);
+      return;
+    }
   }
+  if (side == 64) gemm_reg<T, 64, IK, JK, LIN>(a, s);
+  else gemm_reg<T, 128, IK, JK, LIN>(a, s);
+}
+
+// Work space of the forward pass: copies of x and w with padded rows, and the parts
+struct LinearPlan {
+  bool copy;
+  int64_t ldk;
+  size_t at_w, at_part, bytes;
+};
+static LinearPlan linear_plan(const LinearArgs &a, int dtype) {
+  LinearPlan p{};
+  p.ldk = up(a.k, 32);
+  const Split sp = split_of(a.m, a.n, a.k, dtype, false);
+  // both operands have k along their rows: either's boundaries spoil the product
+  p.copy = copy_pays(dtype, a.m, a.k, a.ldx | a.ldw, a.n, sp.side, 768);
+  size_t off = 0;
+  if (p.copy) off += up((size_t)a.m * p.ldk * 2, 256);
+  p.at_w = off;
+  if (p.copy) off += up((size_t)a.n * p.ldk * 2, 256);
+  p.at_part = off;
+  p.bytes = off + part_bytes(a.m, a.n, a.k, dtype, false);
+  return p;
+}
+
+size_t linear_ws(const LinearArgs &a, int dtype) { return linear_plan(a, dtype).bytes; }
+
+template <class T>
+static LayerMat padded(const void *x, int64_t ld, int64_t m, int d, char *at, hipStream_t s) {
+  const int64_t ldo = up(d, 32), blocks = (m * (ldo / 8) + 255) / 256;
+  hipLaunchKernelGGL(k_pad_rows<T>, dim3((unsigned)(blocks < 1 << 20 ? blocks : 1 << 20)),
+                     dim3(256), 0, s, (const T *)x, ld, m, d, (T *)at, ldo);
+  return LayerMat{at, ldo, 0, nullptr, true};
+}
+
+template <class T>
+static hipError_t linear_t(const LinearArgs &l, int dtype, char *ws, hipStream_t s) {
+  if (l.m <= 0) return hipSuccess;
+  const LinearPlan p = linear_plan(l, dtype);
+  GemmArgs a{};
+  a.I = l.m, a.J = l.n, a.K = l.k;
+  a.A = LayerMat{l.x, l.ldx, 0, nullptr, false};
+  a.B = LayerMat{l.w, l.ldw, 0, nullptr, false};
+  if (p.copy) {
+    if (!direct(a.A, l.k)) a.A = padded<T>(l.x, l.ldx, l.m, l.k, ws, s);
+    if (!direct(a.B, l.k)) a.B = padded<T>(l.w, l.ldw, l.n, l.k, ws + p.at_w, s);
+  }
+  a.lin = l;
+  gemm<T, true, true, true>(a, place<T>(a, (float *)(ws + p.at_part), false), s);
+  if (a.parts > 1)
+    hipLaunchKernelGGL(k_linear_join<T>, dim3((unsigned)join_blocks(a)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
-size_t linear_ws(int64_t m, int n, int k, int dtype) { return part_bytes(m, n, k, dtype); }
-
-template <class T>
-static hipError_t linear_t(const LinearArgs &l, void *ws, hipStream_t s) {
-  GemmArgs a{};
-  a.I = l.m, a.J = l.n, a.K = l.k;
-  a.A = LayerMat{l.x, l.ldx, 0, nullptr};
-  a.B = LayerMat{l.w, l.ldw, 0, nullptr};
-  a.lin = l;
-  return gemm<T, true, true, true>(a, (float *)ws, s);
-}
-
 hipError_t launch_linear(const LinearArgs &a, int dtype, void *ws, hipStream_t s) {
-  if (dtype == NR_F32) return linear_t<float>(a, ws, s);
-  if (dtype == NR_BF16) return linear_t<bf16_t>(a, ws, s);
-  return linear_t<f16_t>(a, ws, s);
+  if (dtype == NR_F32) return linear_t<float>(a, dtype, (char *)ws, s);
+  if (dtype == NR_BF16) return linear_t<bf16_t>(a, dtype, (char *)ws, s);
+  return linear_t<f16_t>(a, dtype, (char *)ws, s);
 }
 
-// Work space of the gradients: dz, the column sums of its blocks, and the
-// products' parts (dx and dw one after the other in the same place)
+// Work space of the gradients: dz, the column sums of its blocks, copies of w and x
+// with padded rows, and the parts of the two products
 struct GradPlan {
   bool act, dz;          // the pass over dy runs; it writes dz
   int64_t rows, nb, ldz; // rows per block of that pass, its blocks, dz's row stride
   int ct;
-  size_t at_part, at_prod, bytes;
+  bool copy_w, copy_x;
+  size_t at_cols, at_cw, at_cx, at_x, at_w, bytes;
 };
 static GradPlan grad_plan(const LinearGradArgs &a, int dtype) {
   GradPlan p{};
-  p.dz = a.act != NR_ACT_NONE && (a.dx || a.dw);
+  const int sx = a.dx ? split_of(a.m, a.k, a.n, dtype, false).side : 0;
+  const int sw = a.dw ? split_of(a.n, a.k, a.m, dtype, true).side : 0;
+  // dz is written where it is another than dy, or dy's rows are off the boundaries
+  p.dz = (a.act != NR_ACT_NONE && (a.dx || a.dw)) ||
+         copy_pays(dtype, a.m, a.n, a.lddy, a.k, sx > sw ? sx : sw, 512);
+  p.copy_w = a.dx && copy_pays(dtype, a.n, a.k, a.ldw, a.m, sx, 512);
+  p.copy_x = a.dw && !a.x.hold && copy_pays(dtype, a.m, a.k, a.x.ld, a.n, sw, 512);
   p.act = p.dz || a.db;
-  p.ct = 1;
+  p.ct = 4;   // whole groups of 32 columns
   while (p.ct < 256 && p.ct * 8 < a.n) p.ct *= 2;
-  const int64_t rt = 256 / p.ct;
-  p.rows = up((a.m + 1023) / 1024, rt);
-  if (p.rows < 8 * rt) p.rows = 8 * rt;
+  // blocks of the pass: some thousand in all, at most 512 of them along the rows
+  const int64_t rt = 256 / p.ct, across = (a.n + 8 * p.ct - 1) / (8 * p.ct);
+  int64_t blocks = 1024 / across;
+  blocks = blocks > 512 ? 512 : blocks;
+  p.rows = up((a.m + blocks - 1) / blocks, 2 * rt);
+  if (p.rows < 2 * rt) p.rows = 2 * rt;
   p.nb = (a.m + p.rows - 1) / p.rows;
   p.ldz = up(a.n, 32);
   size_t off = 0;
   if (p.dz) off += up((size_t)a.m * p.ldz * layer_elem(dtype), 256);
-  p.at_part = off;
+  p.at_cols = off;
   if (a.db) off += up(sizeof(float) * (size_t)p.nb * a.n, 256);
-  p.at_prod = off;
-  const size_t px = a.dx ? part_bytes(a.m, a.k, a.n, dtype) : 0;
-  const size_t pw = a.dw ? part_bytes(a.n, a.k, a.m, dtype) : 0;
-  p.bytes = off + (px > pw ? px : pw);
+  p.at_cw = off;
+  if (p.copy_w) off += up((size_t)a.n * up(a.k, 32) * 2, 256);
+  p.at_cx = off;
+  if (p.copy_x) off += up((size_t)a.m * up(a.k, 32) * 2, 256);
+  p.at_x = off;
+  if (a.dx) off += part_bytes(a.m, a.k, a.n, dtype, false);
+  p.at_w = off;
+  if (a.dw) off += part_bytes(a.n, a.k, a.m, dtype, true);
+  p.bytes = off;
   return p;
 }
 
@@ -769,32 +991,42 @@ template <class T>
 static hipError_t linear_grad_t(const LinearGradArgs &l, int dtype, char *ws, hipStream_t s) {
   const GradPlan p = grad_plan(l, dtype);
   T *dz = p.dz ? (T *)ws : nullptr;
-  float *part = l.db ? (float *)(ws + p.at_part) : nullptr;
-  float *prod = (float *)(ws + p.at_prod);
+  float *cols = l.db ? (float *)(ws + p.at_cols) : nullptr;
   if (p.act && l.m > 0) {
     const dim3 g((unsigned)p.nb, (l.n + 8 * p.ct - 1) / (8 * p.ct));
-    hipLaunchKernelGGL(k_act_grad<T>, g, dim3(256), 0, s, l, p.rows, p.ct, dz, p.ldz, part);
+    hipLaunchKernelGGL(k_act_grad<T>, g, dim3(256), 0, s, l, p.rows, p.ct, dz, p.ldz, cols);
   }
-  hipError_t e = hipGetLastError();
-  if (l.db && e == hipSuccess) e = launch_col_join(part, l.db, nullptr, nullptr, p.nb, l.n, dtype, s);
-  const LayerMat z = p.dz ? LayerMat{dz, p.ldz, 0, nullptr} : LayerMat{l.dy, l.lddy, 0, nullptr};
-  if (l.dx && e == hipSuccess) {
-    GemmArgs a{};
-    a.I = l.m, a.J = l.k, a.K = l.n;
-    a.A = z;
-    a.B = LayerMat{l.w, l.ldw, 0, nullptr};
-    a.out = l.dx, a.ldo = l.lddx;
-    e = gemm<T, true, false, false>(a, prod, s);
+  const LayerMat z = p.dz ? LayerMat{dz, p.ldz, 0, nullptr, true}
+                          : LayerMat{l.dy, l.lddy, 0, nullptr, false};
+  GemmArgs x{}, w{};
+  x.I = l.m, x.J = l.k, x.K = l.n;
+  x.A = z, x.B = LayerMat{l.w, l.ldw, 0, nullptr, false};
+  x.out = l.dx, x.ldo = l.lddx;
+  w.I = l.n, w.J = l.k, w.K = l.m;
+  w.A = z, w.B = l.x;
+  w.out = l.dw, w.ldo = l.lddw;
+  const bool dx = l.dx && l.m > 0, dw = l.dw;
+  const int sx = dx ? place<T>(x, (float *)(ws + p.at_x), false) : 0;
+  const int sw = dw ? place<T>(w, (float *)(ws + p.at_w), true) : 0;
+  if (p.copy_w && l.m > 0 && !direct(x.B, l.k))
+    x.B = padded<T>(l.w, l.ldw, l.n, l.k, ws + p.at_cw, s);
+  if (p.copy_x && l.m > 0 && !direct(w.B, l.k))
+    w.B = padded<T>(l.x.p, l.x.ld, l.m, l.k, ws + p.at_cx, s);
+  if (sx == 64 && sw == 64) {
+    x.grid = tile_grid(x, 64, 64), w.grid = tile_grid(w, 64, 64);
+    const dim3 g((unsigned)(x.grid * x.parts + w.grid * w.parts));
+    if (w.B.hold) hipLaunchKernelGGL((k_gemm_two<T, true>), g, dim3(256), 0, s, x, w);
+    else hipLaunchKernelGGL((k_gemm_two<T, false>), g, dim3(256), 0, s, x, w);
+  } else {
+    if (dx) gemm<T, true, false, false>(x, sx, s);
+    if (dw) gemm<T, false, false, false>(w, sw, s);
   }
-  if (l.dw && e == hipSuccess) {
-    GemmArgs a{};
-    a.I = l.n, a.J = l.k, a.K = l.m;
-    a.A = z;
-    a.B = l.x;
-    a.out = l.dw, a.ldo = l.lddw;
-    e = gemm<T, false, false, false>(a, prod, s);
-  }
-  return e;
+  const int64_t bx = dx ? join_blocks(x) : 0, bw = dw ? join_blocks(w) : 0;
+  const int64_t bc = l.db ? (l.n + 15) / 16 : 0;
+  if (bx + bw + bc > 0)
+    hipLaunchKernelGGL(k_grad_join<T>, dim3((unsigned)(bx + bw + bc)), dim3(256), 0, s, x, w, bx,
+                       bw, cols, p.nb, l.n, (T *)l.db);
+  return hipGetLastError();
 }
 
 hipError_t launch_linear_grad(const LinearGradArgs &a, int dtype, void *ws, hipStream_t s) {

@@ -883,13 +883,24 @@ nr_status check_linear_grad(const nr_linear_grad_desc *d) {
   return check_shape(d->m, d->k, "k");
 }
 
+nr::LinearArgs linear_args(const nr_linear_desc *d) {
+  nr::LinearArgs a{};
+  a.m = d->m, a.n = d->n, a.k = d->k, a.act = d->act;
+  a.x = d->x, a.ldx = d->ldx;
+  a.w = d->w, a.ldw = d->ldw;
+  a.bias = d->bias, a.res = d->residual, a.ldr = d->ldr;
+  a.y = d->y, a.ldy = d->ldy;
+  a.pre = d->pre, a.ldp = d->ldp, a.pre_hold = d->pre_hold, a.pre_scale = d->pre_scale;
+  return a;
+}
+
 nr::LinearGradArgs grad_args(const nr_linear_grad_desc *d) {
   nr::LinearGradArgs a{};
   a.m = d->m, a.n = d->n, a.k = d->k, a.act = d->act;
   a.dy = d->dy, a.lddy = d->lddy;
-  a.x = nr::LayerMat{d->x, d->ldx, d->x_hold, d->x_scale};
+  a.x = nr::LayerMat{d->x, d->ldx, d->x_hold, d->x_scale, false};
   a.w = d->w, a.ldw = d->ldw;
-  a.pre = nr::LayerMat{d->pre, d->ldp, d->pre_hold, d->pre_scale};
+  a.pre = nr::LayerMat{d->pre, d->ldp, d->pre_hold, d->pre_scale, false};
   a.dx = d->dx, a.lddx = d->lddx;
   a.dw = d->dw, a.lddw = d->lddw;
   a.db = d->db;
@@ -905,7 +916,7 @@ nr::NormGradArgs norm_grad_args(const nr_layer_norm_grad_desc *d) {
   nr::NormGradArgs a{};
   a.m = d->m, a.d = d->d;
   a.dy = d->dy, a.lddy = d->lddy;
-  a.x = nr::LayerMat{d->x, d->ldx, d->x_hold, d->x_scale};
+  a.x = nr::LayerMat{d->x, d->ldx, d->x_hold, d->x_scale, false};
   a.mean = d->stats, a.rstd = d->stats ? d->stats + d->m : nullptr;
   a.g = d->weight, a.add = d->add, a.ldadd = d->ldadd;
   a.dx = d->dx, a.lddx = d->lddx;
@@ -1449,7 +1460,7 @@ nr_status nr_act_read(const void *q, const uint8_t *scale, int64_t m, int32_t d,
 }
 
 size_t nr_linear_ws(const nr_linear_desc *d) {
-  return check_linear(d) == NR_OK ? nr::linear_ws(d->m, d->n, d->k, d->dtype) : 0;
+  return check_linear(d) == NR_OK ? nr::linear_ws(linear_args(d), d->dtype) : 0;
 }
 
 nr_status nr_linear(const nr_linear_desc *d, void *ws, size_t ws_bytes, hipStream_t stream) {
@@ -1463,15 +1474,9 @@ nr_status nr_linear(const nr_linear_desc *d, void *ws, size_t ws_bytes, hipStrea
     NR_TRY(check_held(d->pre, d->pre_scale, d->ldp, d->m, d->n, d->pre_hold, "pre"));
   else if (d->pre)
     NR_TRY(check_mat(d->pre, d->ldp, d->m, d->n, d->dtype, "pre"));
-  NR_TRY(check_ws(ws, ws_bytes, nr::linear_ws(d->m, d->n, d->k, d->dtype)));
+  const nr::LinearArgs a = linear_args(d);
+  NR_TRY(check_ws(ws, ws_bytes, nr::linear_ws(a, d->dtype)));
   if (d->m == 0) return NR_OK;
-  nr::LinearArgs a{};
-  a.m = d->m, a.n = d->n, a.k = d->k, a.act = d->act;
-  a.x = d->x, a.ldx = d->ldx;
-  a.w = d->w, a.ldw = d->ldw;
-  a.bias = d->bias, a.res = d->residual, a.ldr = d->ldr;
-  a.y = d->y, a.ldy = d->ldy;
-  a.pre = d->pre, a.ldp = d->ldp, a.pre_hold = d->pre_hold, a.pre_scale = d->pre_scale;
   HIP_OK(nr::launch_linear(a, d->dtype, ws, stream));
   return NR_OK;
 }

@@ -19,6 +19,7 @@ struct LayerMat {
   int64_t ld;            // elements of the type, or bytes of q
   int hold;
   const uint8_t *scale;  // [rows x ld / 32] when held
+  bool padded;           // zeros from the width up to ld
 };
 
 struct LinearArgs {
@@ -84,7 +85,7 @@ struct NormGradArgs {
   void *dg, *db;
 };
 
-size_t linear_ws(int64_t m, int n, int k, int dtype);
+size_t linear_ws(const LinearArgs &a, int dtype);
 hipError_t launch_linear(const LinearArgs &a, int dtype, void *ws, hipStream_t s);
 size_t linear_grad_ws(const LinearGradArgs &a, int dtype);
 hipError_t launch_linear_grad(const LinearGradArgs &a, int dtype, void *ws, hipStream_t s);
