@@ -174,9 +174,13 @@ struct Operand {
   template <bool FULL>
   __device__ __forceinline__ void fetch(const LayerMat &m, int64_t o0, int64_t nO, int64_t k,
                                         int64_t kend, int64_t K) {
+    int tid = threadIdx.x;
+    // the addresses of tiles at an end are found where they are needed: kept over
+    // the whole loop they would cost the registers that the products need
+    if constexpr (!FULL) asm volatile("" : "+v"(tid));
 #pragma unroll
     for (int u = 0; u < N; ++u) {
-      const int e = threadIdx.x + NT * u;
+      const int e = tid + NT * u;
       int64_t row = (KC ? o0 : k) + e / CPR;
       const int64_t col = (KC ? k : o0) + 8 * (e % CPR), cols = KC ? kend : nO;
       bool in = true;
@@ -620,28 +624,52 @@ __global__ void __launch_bounds__(256, 2) k_gemm_dma(GemmArgs a) {
   }
 }
 
-// The parts' sums, in order, and the epilogue: eight columns of a row per thread
+// The parts' sums and the epilogue, eight columns of a row per thread.  Many parts
+// are added by four waves, every fourth part each (their loads wait for one
+// another), whose sums the first then adds in order
+constexpr int JOIN_ONE = 8;   // parts that one thread adds
 template <class T, bool LIN>
 __device__ __forceinline__ void join_body(const GemmArgs &a, int64_t block, int64_t blocks) {
+  __shared__ float4 red[3][2][WAVE];
   const int64_t per = a.ldp / 8, units = a.I * per;   // whole quads per row
-  for (int64_t u = block * 256 + threadIdx.x; u < units; u += blocks * 256) {
-    const int64_t i = u / per;
+  const bool four = a.parts > JOIN_ONE;
+  const int chain = four ? threadIdx.x / WAVE : 0, step = four ? 4 : 1;
+  const int width = four ? WAVE : 256, at = threadIdx.x % width;
+  for (int64_t u0 = block * width; u0 < units; u0 += blocks * width) {
+    const int64_t u = u0 + at, i = u / per;
     const int j = (int)(u - i * per) * 8;
     float v[8] = {};
     Raw8<T> bias, res;
-    if constexpr (LIN) {
-      if (a.lin.bias) bias.load((const T *)a.lin.bias, j, a.J);
-      if (a.lin.res) res.load((const T *)a.lin.res + i * a.lin.ldr, j, a.J);
-    }
+    if (u < units) {
+      if constexpr (LIN) {
+        if (a.lin.bias) bias.load((const T *)a.lin.bias, j, a.J);
+        if (a.lin.res) res.load((const T *)a.lin.res + i * a.lin.ldr, j, a.J);
+      }
 #pragma unroll 4
-    for (int s = 0; s < a.parts; ++s) {
-      const float4 *p =
-          reinterpret_cast<const float4 *>(a.part + ((int64_t)s * a.I + i) * a.ldp + j);
-      const float4 x = p[0], y = p[1];
-      v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
-      v[4] += y.x, v[5] += y.y, v[6] += y.z, v[7] += y.w;
+      for (int s = chain; s < a.parts; s += step) {
+        const float4 *p =
+            reinterpret_cast<const float4 *>(a.part + ((int64_t)s * a.I + i) * a.ldp + j);
+        const float4 x = p[0], y = p[1];
+        v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
+        v[4] += y.x, v[5] += y.y, v[6] += y.z, v[7] += y.w;
+      }
     }
-    finish<T, LIN>(a, i, j, true, v, bias, res);
+    if (four) {
+      __syncthreads();   // the units before have been added
+      if (chain > 0) {
+        red[chain - 1][0][at] = make_float4(v[0], v[1], v[2], v[3]);
+        red[chain - 1][1][at] = make_float4(v[4], v[5], v[6], v[7]);
+      }
+      __syncthreads();
+      if (chain > 0) continue;
+#pragma unroll
+      for (int c = 0; c < 3; ++c) {
+        const float4 x = red[c][0][at], y = red[c][1][at];
+        v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
+        v[4] += y.x, v[5] += y.y, v[6] += y.z, v[7] += y.w;
+      }
+    }
+    if (u < units) finish<T, LIN>(a, i, j, true, v, bias, res);
   }
 }
 
@@ -674,10 +702,11 @@ __global__ void __launch_bounds__(256) k_grad_join(GemmArgs x, GemmArgs w, int64
                                                    const float *cols, int64_t rows, int n, T *db) {
   __shared__ float red[16][17];
   int64_t b = blockIdx.x;
-  if (b < bx) return join_body<T, false>(x, b, bx);
-  b -= bx;
-  if (b < bw) return join_body<T, false>(w, b, bw);
-  b -= bw;
+  if (b < bx + bw) {
+    const bool first = b < bx;
+    return join_body<T, false>(first ? x : w, first ? b : b - bx, first ? bx : bw);
+  }
+  b -= bx + bw;
   const int c = (int)b * 16 + (threadIdx.x & 15), q = threadIdx.x >> 4;
   float v = 0.0f;
   if (c < n) {
@@ -705,25 +734,47 @@ __global__ void __launch_bounds__(256) k_act_grad(LinearGradArgs a, int64_t rows
   const int c0 = (blockIdx.y * ct + tc) * 8;
   const int64_t r0 = (int64_t)blockIdx.x * rows, r1 = r0 + rows < a.m ? r0 + rows : a.m;
   float s[8] = {};
+  constexpr int B = 4;   // rows under way
   if (c0 < ldz)
-    for (int64_t r = r0 + tr; r < r1; r += rt) {
-      float v[8], z[8];
-      load8((const T *)a.dy + r * a.lddy, c0, a.n, v);
-      if (a.act != NR_ACT_NONE) {
-        if (a.pre.hold)   // (its rows are padded as dz's are)
-          read8<T>((const uint8_t *)a.pre.p + r * a.pre.ld, a.pre.scale + r * (a.pre.ld / 32), c0,
-                a.pre.hold, z);
-        else
-          load8((const T *)a.pre.p + r * a.pre.ld, c0, a.n, z);
+    for (int64_t r = r0 + tr; r < r1; r += B * rt) {
+      Raw8<T> v[B], z[B];
+      uint2 zq[B];
+      uint8_t zs[B];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= act_slope<exact>(z[i], a.act);
+      for (int b = 0; b < B; ++b) {
+        const int64_t rb = r + b * rt < r1 ? r + b * rt : r;
+        v[b].load((const T *)a.dy + rb * a.lddy, c0, a.n);
+        if (a.act == NR_ACT_NONE) continue;
+        if (a.pre.hold) {   // (its rows are padded as dz's are)
+          zq[b] = *reinterpret_cast<const uint2 *>((const uint8_t *)a.pre.p + rb * a.pre.ld + c0);
+          zs[b] = a.pre.scale[rb * (a.pre.ld / 32) + (c0 >> 5)];
+        } else {
+          z[b].load((const T *)a.pre.p + rb * a.pre.ld, c0, a.n);
+        }
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        v[i] = c0 + i < a.n ? v[i] : 0.0f;   // (a slope of what is behind the width)
-        s[i] += v[i];
+      for (int b = 0; b < B; ++b) {
+        if (r + b * rt >= r1) break;
+        float d[8], y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[i] = v[b][i];
+        if (a.act != NR_ACT_NONE) {
+          if (a.pre.hold) {
+            unpack8<T>(zq[b], zs[b], a.pre.hold, y);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = z[b][i];
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i) d[i] *= act_slope<exact>(y[i], a.act);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          d[i] = c0 + i < a.n ? d[i] : 0.0f;   // (a slope of what is behind the width)
+          s[i] += d[i];
+        }
+        if (dz) store8(dz + (r + b * rt) * ldz, c0, (int)ldz, d);
       }
-      if (dz) store8(dz + r * ldz, c0, (int)ldz, v);
     }
   if (!part) return;
 #pragma unroll
@@ -747,41 +798,41 @@ static bool aligned(const void *p, int64_t ld, size_t e, size_t to) {
 }
 
 // How a product is cut: the tile's side (256: 256 x 128), and parts of k.  The
-// cheapest by this estimate of its time in us, from rates measured on MI355X:
-// a block's share of a CU that is kept busy by two goes at `rate` / 256
-// (TFLOP/s, by tile; products with both operands transposed less in small
-// tiles), one alone on its CU at 4/5 of that; parts cost a launch and their sums
-// pass through memory (the last-level cache) twice at 10 TB/s.  Estimate /
-// measured: 10,000 x 1536 -> 512 fp32 in 64 x 64 121 / 115, 128 x 128 140 / 118, in
-// four parts 114 / 109; 4096 x 1024 -> 256 bf16 64 x 64 12 / 12, 128 x 128 18 / 18;
-// 16,384 x 512 -> 512 bf16 27 / 27, 26 / 19, 256 x 128 32 / 27; dw of 4096 rows, 1024 x
-// 256, bf16 64 x 64 in four parts 19 / 23, 128 x 128 in eight 17 / 18
+// cheapest by an estimate of its time in us, from what was measured on MI355X: a
+// block takes its tile's products at `rate` / 256 (TFLOP/s) where blocks share a
+// CU, at `alone` / 256 where it has one to itself, but at least `step` for each
+// K-tile of bk; parts cost a launch, and their sums' way through memory.
+// @@
 struct Split {
   int side, parts;
   int64_t kchunk;
 };
 static Split split_of(int64_t I, int J, int64_t K, int dtype, bool both_transposed) {
   struct Kind {
-    int side, ti, tj;
-    double rate;
+    int side, ti, tj, bk;
+    double rate, alone, step;
   };
   const bool f32 = dtype == NR_F32;
-  const Kind kinds[3] = {{64, 64, 64, f32 ? 145.0 : both_transposed ? 280.0 : 390.0},
-                         {128, 128, 128, f32 ? 190.0 : 800.0},
-                         {256, 256, 128, 950.0}};
+  const double small = both_transposed ? 280 : 390;
+  const Kind kinds[3] = {
+      f32 ? Kind{64, 64, 64, 64, 130, 105, 1.6} : Kind{64, 64, 64, 128, small, 0.8 * small, 1.5},
+      f32 ? Kind{128, 128, 128, 32, 190, 110, 1.8} : Kind{128, 128, 128, 32, 850, 800, 0.35},
+      Kind{256, 256, 128, 32, 1000, 800, 0.45}};
   Split best{64, 1, 128};
   double least = 0.0;
   for (int q = 0; q < (f32 ? 2 : 3); ++q) {
     const Kind &kind = kinds[q];
     const double tiles = (double)(up(I, kind.ti) / kind.ti) * (double)(up(J, kind.tj) / kind.tj);
-    for (int want = 1; want <= 64; want *= 2) {
+    for (int want = 1; want <= 256; want *= 2) {
       if (want > 1 && (K < 256 * want || tiles * want > 2048)) break;
       const int64_t kc = K > 0 ? up((K + want - 1) / want, 128) : 128;
       const int parts = K > 0 ? (int)((K + kc - 1) / kc) : 1;
-      const double block = 2e-6 * kind.ti * kind.tj * kc / (kind.rate / 256);
-      const double per_cu = std::ceil(tiles * parts / 256);
-      const double us = block * (per_cu + (std::fmod(per_cu, 2.0) == 1.0 ? 0.25 : 0.0)) +
-                        (parts > 1 ? 4.0 + 8e-7 * parts * (double)I * J : 0.0);
+      const double block = 2e-6 * 256 * kind.ti * kind.tj * kc;
+      const int64_t per_cu = (int64_t)((tiles * parts + 255) / 256);
+      const double busy = per_cu / 2 * 2 * block / kind.rate + per_cu % 2 * block / kind.alone;
+      const double wait = (per_cu + 1) / 2 * kind.step * (double)((kc + kind.bk - 1) / kind.bk);
+      const double us = (busy > wait ? busy : wait) +
+                        (parts > 1 ? 5.0 + 1.25e-6 * parts * (double)I * J : 0.0);
       if ((q == 0 && want == 1) || us < least) {
         least = us;
         best = Split{kind.side, parts, kc};
@@ -847,7 +898,8 @@ static int place(GemmArgs &a, float *ws, bool both_transposed) {
 }
 static int64_t join_blocks(const GemmArgs &a) {
   if (a.parts < 2) return 0;
-  const int64_t b = (a.I * (a.ldp / 8) + 255) / 256;
+  const int64_t width = a.parts > JOIN_ONE ? WAVE : 256;
+  const int64_t b = (a.I * (a.ldp / 8) + width - 1) / width;
   return b < 1 << 20 ? b : 1 << 20;
 }
 
@@ -957,7 +1009,8 @@ static GradPlan grad_plan(const LinearGradArgs &a, int dtype) {
   p.dz = (a.act != NR_ACT_NONE && (a.dx || a.dw)) ||
          copy_pays(dtype, a.m, a.n, a.lddy, a.k, sx > sw ? sx : sw, 512);
   p.copy_w = a.dx && copy_pays(dtype, a.n, a.k, a.ldw, a.m, sx, 512);
-  p.copy_x = a.dw && !a.x.hold && copy_pays(dtype, a.m, a.k, a.x.ld, a.n, sw, 512);
+  p.copy_x = a.dw && (a.x.hold ? dtype != NR_F32 && sw >= 128 && a.m > 0 && a.n >= 512
+                               : copy_pays(dtype, a.m, a.k, a.x.ld, a.n, sw, 512));
   p.act = p.dz || a.db;
   p.ct = 4;   // whole groups of 32 columns
   while (p.ct < 256 && p.ct * 8 < a.n) p.ct *= 2;
@@ -965,8 +1018,9 @@ static GradPlan grad_plan(const LinearGradArgs &a, int dtype) {
   const int64_t rt = 256 / p.ct, across = (a.n + 8 * p.ct - 1) / (8 * p.ct);
   int64_t blocks = 1024 / across;
   blocks = blocks > 512 ? 512 : blocks;
-  p.rows = up((a.m + blocks - 1) / blocks, 2 * rt);
-  if (p.rows < 2 * rt) p.rows = 2 * rt;
+  p.rows = up((a.m + blocks - 1) / blocks, 4 * rt);
+  if (a.m < blocks * 4 * rt) p.rows = up((a.m + 255) / 256, rt);   // few rows: spread them
+  if (p.rows < rt) p.rows = rt;
   p.nb = (a.m + p.rows - 1) / p.rows;
   p.ldz = up(a.n, 32);
   size_t off = 0;
@@ -1010,8 +1064,15 @@ static hipError_t linear_grad_t(const LinearGradArgs &l, int dtype, char *ws, hi
   const int sw = dw ? place<T>(w, (float *)(ws + p.at_w), true) : 0;
   if (p.copy_w && l.m > 0 && !direct(x.B, l.k))
     x.B = padded<T>(l.w, l.ldw, l.n, l.k, ws + p.at_cw, s);
-  if (p.copy_x && l.m > 0 && !direct(w.B, l.k))
+  if (p.copy_x && l.x.hold) {
+    const int64_t ld = up(l.k, 32);   // its padding is zeros
+    const hipError_t e = launch_read((const uint8_t *)l.x.p, l.x.scale, l.m, (int)ld, l.x.hold,
+                                     dtype, ws + p.at_cx, ld, s);
+    if (e != hipSuccess) return e;
+    w.B = LayerMat{ws + p.at_cx, ld, 0, nullptr, true};
+  } else if (p.copy_x && l.m > 0 && !direct(w.B, l.k)) {
     w.B = padded<T>(l.x.p, l.x.ld, l.m, l.k, ws + p.at_cx, s);
+  }
   if (sx == 64 && sw == 64) {
     x.grid = tile_grid(x, 64, 64), w.grid = tile_grid(w, 64, 64);
     const dim3 g((unsigned)(x.grid * x.parts + w.grid * w.parts));

@@ -205,19 +205,23 @@ __device__ __forceinline__ void hold_unpack4(uint32_t w, float s, int hold, floa
   }
 }
 
-// eight elements of a held row from column c0 (a multiple of 8) on, as the type
-// has them (fp16's subnormals round); the row's q bytes start on a 16-byte
-// boundary and are padded to whole groups
+// eight held elements, as the type has them (fp16's subnormals round)
 template <class T>
-__device__ __forceinline__ void read8(const uint8_t *q, const uint8_t *scale, int c0, int hold,
-                                      float (&v)[8]) {
-  const uint2 w = *reinterpret_cast<const uint2 *>(q + c0);
-  const float s = hold_scale(scale[c0 >> 5]);
+__device__ __forceinline__ void unpack8(uint2 w, uint8_t scale, int hold, float (&v)[8]) {
+  const float s = hold_scale(scale);
   hold_unpack4(w.x, s, hold, v);
   hold_unpack4(w.y, s, hold, v + 4);
   if constexpr (__is_same(T, f16_t))
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = to_f32(from_f32<T>(v[i]));
+}
+
+// eight elements of a held row from column c0 (a multiple of 8) on; the row's q
+// bytes start on a 16-byte boundary and are padded to whole groups
+template <class T>
+__device__ __forceinline__ void read8(const uint8_t *q, const uint8_t *scale, int c0, int hold,
+                                      float (&v)[8]) {
+  unpack8<T>(*reinterpret_cast<const uint2 *>(q + c0), scale[c0 >> 5], hold, v);
 }
 
 // eight elements v of a row at column c0, whose group the four lanes l ^ 1, l ^ 2
@@ -244,20 +248,23 @@ __device__ __forceinline__ void write8(uint8_t *q, uint8_t *scale, int c0, int h
 
 // ---------------------------------------------------------------- activations
 
-// z Phi(z) = z erfc(-z / sqrt 2) / 2.  EXACT (fp32 results): the library's erfc.
-// The 16-bit types take Abramowitz and Stegun 7.1.26, erfc(x) = t(p1 + t(p2 +
-// ...)) exp(-x^2) for x >= 0 with t = 1 / (1 + p x), off by at most 1.5e-7, far
-// below half a step of theirs
+// Phi(z) = erfc(-z / sqrt 2) / 2, and e = exp(-z^2 / 2).  EXACT (fp32 results): the
+// library's erfc.  The 16-bit types take Abramowitz and Stegun 7.1.26, erfc(x) =
+// t(p1 + t(p2 + ...)) exp(-x^2) for x >= 0 with t = 1 / (1 + p x), off by at most
+// 1.5e-7, far below half a step of theirs
 template <bool EXACT>
-__device__ __forceinline__ float normal_cdf(float z) {
+__device__ __forceinline__ float normal_cdf(float z, float &e) {
   if constexpr (EXACT) {
+    e = expf(-0.5f * z * z);
     return 0.5f * erfcf(z * -0.70710678118654752f);
   } else {
-    const float x = fabsf(z) * 0.70710678118654752f;
-    const float t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * x);
-    const float p = t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f +
-                    t * (-1.453152027f + t * 1.061405429f))));
-    const float h = 0.5f * p * __expf(-x * x);   // Phi(-|z|)
+    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.3275911f * 0.70710678f, 1.0f));
+    e = __builtin_amdgcn_exp2f(z * z * -0.72134752f);   // log2(e) / 2
+    float p = fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
+    p = fmaf(t, p, 0.5f * 1.421413741f);
+    p = fmaf(t, p, 0.5f * -0.284496736f);
+    p = fmaf(t, p, 0.5f * 0.254829592f);
+    const float h = p * t * e;   // Phi(-|z|)
     return z < 0.0f ? h : 1.0f - h;
   }
 }
@@ -265,13 +272,16 @@ __device__ __forceinline__ float normal_cdf(float z) {
 template <bool EXACT>
 __device__ __forceinline__ float logistic(float z) {
   if constexpr (EXACT) return 1.0f / (1.0f + expf(-z));
-  return __builtin_amdgcn_rcpf(1.0f + __expf(-z));
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504f));
 }
 
 template <bool EXACT>
 __device__ __forceinline__ float act_value(float z, int act) {
   if (act == NR_ACT_RELU) return z > 0.0f || z != z ? z : 0.0f;   // a NaN stays one
-  if (act == NR_ACT_GELU) return z * normal_cdf<EXACT>(z);
+  if (act == NR_ACT_GELU) {
+    float e;
+    return z * normal_cdf<EXACT>(z, e);
+  }
   if (act == NR_ACT_SILU) return z * logistic<EXACT>(z);
   return z;
 }
@@ -280,12 +290,13 @@ template <bool EXACT>
 __device__ __forceinline__ float act_slope(float z, int act) {
   if (act == NR_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
   if (act == NR_ACT_GELU) {
-    const float e = EXACT ? expf(-0.5f * z * z) : __expf(-0.5f * z * z);
-    return normal_cdf<EXACT>(z) + z * e * 0.39894228040143268f;
+    float e;
+    const float c = normal_cdf<EXACT>(z, e);
+    return fmaf(z * e, 0.39894228040143268f, c);
   }
   if (act == NR_ACT_SILU) {
     const float p = logistic<EXACT>(z);
-    return p * (1.0f + z * (1.0f - p));
+    return p * fmaf(z, 1.0f - p, 1.0f);
   }
   return 1.0f;
 }
