@@ -22,7 +22,7 @@ struct GemmArgs {
   int64_t I, K, kchunk;  // k of a part, a multiple of the K-tiles
   int J;
   LayerMat A, B;         // B may be held in 8 bits where j runs along its rows
-  int64_t grid;          // blocks per part
+  int64_t grid;          // blocks, a multiple of 8
   int parts;
   float *part;           // [parts][I][ldp] sums of the parts, or NULL
   int64_t ldp;
@@ -429,7 +429,8 @@ __device__ __forceinline__ void multiply(const char *la, const char *lb, int wi,
 // A block of 256 threads owns a TI x TJ tile, each wave a quarter of it in
 // blocks of 16 x 16.  The next K-tile is read into registers while this one is
 // multiplied.  Blocks go to the eight XCDs in turn: each XCD takes a run of
-// neighbouring tiles, so that their operands meet in its L2.
+// neighbouring tiles, of one part of k after the other, so that their operands
+// meet in its L2.
 // Tiles of 64 x 64 take K-tiles twice as long: what they lack is loads under way.
 template <class T, int S>
 struct RegTile {
@@ -446,15 +447,14 @@ __device__ __forceinline__ void gemm_body(const GemmArgs &a, char *lds, int64_t 
   const int lane = lane_id(), wave = threadIdx.x / WAVE;
   const int wi = TI / 2 * (wave & 1), wj = TJ / 2 * (wave >> 1);
   const int64_t ti = (a.I + TI - 1) / TI, tj = (a.J + TJ - 1) / TJ, tiles = ti * tj;
-  const int64_t per = (tiles + 7) / 8;
-  const int part = (int)(block / a.grid);
-  const int64_t k0 = part * a.kchunk;
-  const int64_t k1 = k0 + a.kchunk < a.K ? k0 + a.kchunk : a.K;
-  for (int64_t u = block - part * a.grid; u < 8 * per; u += a.grid) {
-    const int64_t t = (u & 7) * per + (u >> 3);
-    if (t >= tiles) continue;   // the whole block together
+  const int64_t units = tiles * a.parts, per = (units + 7) / 8;
+  for (int64_t u = block; u < 8 * per; u += a.grid) {
+    const int64_t unit = (u & 7) * per + (u >> 3);
+    if (unit >= units) continue;   // the whole block together
+    const int part = (int)(unit / tiles);
+    const int64_t k0 = part * a.kchunk, k1 = k0 + a.kchunk < a.K ? k0 + a.kchunk : a.K;
     int64_t i0, j0;
-    tile_at(t, ti, tj, i0, j0);
+    tile_at(unit - part * tiles, ti, tj, i0, j0);
     i0 *= TI, j0 *= TJ;
     const bool inside = i0 + TI <= a.I && j0 + TJ <= a.J;
     OA fa;
@@ -511,9 +511,8 @@ __global__ void __launch_bounds__(256, 2) k_gemm(GemmArgs a) {
 template <class T, bool HELD>
 __global__ void __launch_bounds__(256, 2) k_gemm_two(GemmArgs x, GemmArgs w) {
   __shared__ __attribute__((aligned(16))) char lds[RegTile<T, 64>::BYTES];
-  const int64_t nw = w.grid * w.parts;
-  if (blockIdx.x < nw) gemm_body<T, 64, false, false, HELD, false>(w, lds, blockIdx.x);
-  else gemm_body<T, 64, true, false, false, false>(x, lds, blockIdx.x - nw);
+  if (blockIdx.x < w.grid) gemm_body<T, 64, false, false, HELD, false>(w, lds, blockIdx.x);
+  else gemm_body<T, 64, true, false, false, false>(x, lds, blockIdx.x - w.grid);
 }
 
 // The same for 16-bit operands whose rows lie on 16-byte boundaries: K-tiles go
@@ -532,10 +531,9 @@ __global__ void __launch_bounds__(256, 2) k_gemm_dma(GemmArgs a) {
   const int wave = threadIdx.x / WAVE;
   const int wi = TI / 2 * (wave & 1), wj = TJ / 2 * (wave >> 1);
   const int64_t ti = (a.I + TI - 1) / TI, tj = (a.J + TJ - 1) / TJ, tiles = ti * tj;
-  const int64_t per = (tiles + 7) / 8;
-  const int part = (int)(blockIdx.x / a.grid);
-  const int64_t k0 = part * a.kchunk;
-  const int64_t k1 = k0 + a.kchunk < a.K ? k0 + a.kchunk : a.K;
+  const int64_t units = tiles * a.parts, per = (units + 7) / 8;
+  int part = 0;
+  int64_t k0 = 0, k1 = 0;       // the unit's
   int in = 0, out = 0;          // LDS buffers to fill and to read next
   int64_t i0 = 0, j0 = 0, left = 0;   // the tile; k of it not yet asked for
   uint32_t oa[OA::N], ob[OB::N];
@@ -554,22 +552,26 @@ __global__ void __launch_bounds__(256, 2) k_gemm_dma(GemmArgs a) {
     if (left >= BK) fetch(std::true_type{});
     else if (left > 0) fetch(std::false_type{});
   };
-  // the block's next tile from its u-th on (-1: none left), its first two K-tiles
+  // the block's next unit from its u-th on (-1: none left), its first two K-tiles
   // asked for
   auto begin = [&](int64_t u) -> int64_t {
-    for (; u < 8 * per; u += a.grid)
-      if ((u & 7) * per + (u >> 3) < tiles) {
-        tile_at((u & 7) * per + (u >> 3), ti, tj, i0, j0);
-        i0 *= TI, j0 *= TJ;
-        OA::dma_offsets(a.A, i0, a.I, oa);
-        OB::dma_offsets(a.B, j0, a.J, ob);
-        pa = (const T *)a.A.p + (IK ? i0 * a.A.ld + k0 : k0 * a.A.ld + i0);
-        pb = (const T *)a.B.p + (JK ? j0 * a.B.ld + k0 : k0 * a.B.ld + j0);
-        left = k1 - k0;
-        fetch_any();
-        fetch_any();
-        return u;
-      }
+    for (; u < 8 * per; u += a.grid) {
+      const int64_t unit = (u & 7) * per + (u >> 3);
+      if (unit >= units) continue;
+      part = (int)(unit / tiles);
+      k0 = part * a.kchunk;
+      k1 = k0 + a.kchunk < a.K ? k0 + a.kchunk : a.K;
+      tile_at(unit - part * tiles, ti, tj, i0, j0);
+      i0 *= TI, j0 *= TJ;
+      OA::dma_offsets(a.A, i0, a.I, oa);
+      OB::dma_offsets(a.B, j0, a.J, ob);
+      pa = (const T *)a.A.p + (IK ? i0 * a.A.ld + k0 : k0 * a.A.ld + i0);
+      pb = (const T *)a.B.p + (JK ? j0 * a.B.ld + k0 : k0 * a.B.ld + j0);
+      left = k1 - k0;
+      fetch_any();
+      fetch_any();
+      return u;
+    }
     return -1;
   };
   // the wave's own reads into LDS are done but for the last `but`, its reads of
@@ -581,8 +583,7 @@ __global__ void __launch_bounds__(256, 2) k_gemm_dma(GemmArgs a) {
   };
   std::integral_constant<int, 0> ALL;
   std::integral_constant<int, OA::N + OB::N> BUT_LAST;
-  const int64_t nk = (k1 - k0 + BK - 1) / BK;
-  int64_t u = begin(blockIdx.x - part * a.grid);
+  int64_t u = begin(blockIdx.x);
   while (u >= 0) {
     v4f acc[NI][NJ];
 #pragma unroll
@@ -601,6 +602,7 @@ __global__ void __launch_bounds__(256, 2) k_gemm_dma(GemmArgs a) {
 #pragma unroll
         for (int j = 0; j < NJ; ++j) acc[i][j] = mma(fj[j], fi[i], acc[i][j]);
     };
+    const int64_t nk = (k1 - k0 + BK - 1) / BK;
     int64_t n = 0;
     while (left >= BK) {   // a whole K-tile is still to be asked for
       arrived(BUT_LAST);
@@ -616,10 +618,11 @@ __global__ void __launch_bounds__(256, 2) k_gemm_dma(GemmArgs a) {
     arrived(ALL);   // the last K-tile has been read
     // the next tile's first K-tiles come while this one is finished; the third
     // buffer is free for that
-    const int64_t i1 = i0 + wi, j1 = j0 + wj;
+    const int64_t i1 = i0 + wi, j1 = j0 + wj, ka = k0, kb = k1;
+    const int done = part;
     u = begin(u + a.grid);
-    write_tile<T, NI, NJ, IK, JK, false, LIN>(a, acc, lds + in + wave * 1024 * NJ, i1, j1, part,
-                                              k0, k1);
+    write_tile<T, NI, NJ, IK, JK, false, LIN>(a, acc, lds + in + wave * 1024 * NJ, i1, j1, done,
+                                              ka, kb);
     __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): nothing is under way into registers
   }
 }
@@ -882,7 +885,7 @@ static bool copy_pays(int dtype, int64_t rows, int64_t width, int64_t ld, int64_
 }
 
 static int64_t tile_grid(const GemmArgs &a, int ti, int tj) {
-  const int64_t n = up(up(a.I, ti) / ti * (up(a.J, tj) / tj), 8);
+  const int64_t n = up(up(a.I, ti) / ti * (up(a.J, tj) / tj) * a.parts, 8);
   return n < 1 << 20 ? n : 1 << 20;   // blocks take further tiles in turn
 }
 
@@ -906,7 +909,7 @@ static int64_t join_blocks(const GemmArgs &a) {
 template <class T, int S, bool IK, bool JK, bool LIN>
 static void gemm_reg(GemmArgs &a, hipStream_t s) {
   a.grid = tile_grid(a, S, S);
-  const dim3 g((unsigned)(a.grid * a.parts));
+  const dim3 g((unsigned)a.grid);
   if constexpr (!IK) {
     if (a.B.hold) {
       hipLaunchKernelGGL((k_gemm<T, S, IK, JK, true, LIN>), g, dim3(256), 0, s, a);
@@ -921,10 +924,9 @@ static void gemm(GemmArgs &a, int side, hipStream_t s) {
   if (a.I <= 0) return;
   if constexpr (sizeof(T) == 2) {
     if (side >= 128 && direct(a.A, IK ? a.K : a.I) && direct(a.B, JK ? a.K : a.J)) {
-      const int64_t room = up(512 / a.parts > 0 ? 512 / a.parts : 1, 8);   // two blocks a CU
       const int64_t n = tile_grid(a, side, 128);
-      a.grid = n < room ? n : room;
-      const dim3 g((unsigned)(a.grid * a.parts));
+      a.grid = n < 512 ? n : 512;   // two blocks a CU
+      const dim3 g((unsigned)a.grid);
       if (side == 256)
         hipLaunchKernelGGL((k_gemm_dma<T, 256, 128, IK, JK, LIN>), g, dim3(256), 0, s, a);
       else
@@ -1075,7 +1077,7 @@ static hipError_t linear_grad_t(const LinearGradArgs &l, int dtype, char *ws, hi
   }
   if (sx == 64 && sw == 64) {
     x.grid = tile_grid(x, 64, 64), w.grid = tile_grid(w, 64, 64);
-    const dim3 g((unsigned)(x.grid * x.parts + w.grid * w.parts));
+    const dim3 g((unsigned)(x.grid + w.grid));
     if (w.B.hold) hipLaunchKernelGGL((k_gemm_two<T, true>), g, dim3(256), 0, s, x, w);
     else hipLaunchKernelGGL((k_gemm_two<T, false>), g, dim3(256), 0, s, x, w);
   } else {
