@@ -519,9 +519,9 @@ __global__ void __launch_bounds__(256, 2) k_gemm_two(GemmArgs x, GemmArgs w) {
 // straight from memory into LDS, two ahead of the products.  256 x 128 tiles by
 // four waves: two blocks share a CU, and one reads its operands from LDS, or makes
 // its epilogue, while the other multiplies
-template <class T, int TI, int TJ, bool IK, bool JK, bool LIN>
+template <class T, int TI, int TJ, int BK, int NB, bool IK, bool JK, bool LIN>
 __global__ void __launch_bounds__(256, 2) k_gemm_dma(GemmArgs a) {
-  constexpr int BK = 32, NB = 3, NI = TI / 32, NJ = TJ / 32;
+  constexpr int NI = TI / 32, NJ = TJ / 32;
   typedef Operand<T, TI, IK, false, 256, BK> OA;
   typedef Operand<T, TJ, JK, false, 256, BK> OB;
   typedef typename OA::E8 E8;
@@ -568,8 +568,8 @@ __global__ void __launch_bounds__(256, 2) k_gemm_dma(GemmArgs a) {
       pa = (const T *)a.A.p + (IK ? i0 * a.A.ld + k0 : k0 * a.A.ld + i0);
       pb = (const T *)a.B.p + (JK ? j0 * a.B.ld + k0 : k0 * a.B.ld + j0);
       left = k1 - k0;
-      fetch_any();
-      fetch_any();
+#pragma unroll
+      for (int b = 1; b < NB; ++b) fetch_any();
       return u;
     }
     return -1;
@@ -582,7 +582,7 @@ __global__ void __launch_bounds__(256, 2) k_gemm_dma(GemmArgs a) {
     asm volatile("" ::: "memory");
   };
   std::integral_constant<int, 0> ALL;
-  std::integral_constant<int, OA::N + OB::N> BUT_LAST;
+  std::integral_constant<int, (NB - 2) * (OA::N + OB::N)> BUT_LAST;
   int64_t u = begin(blockIdx.x);
   while (u >= 0) {
     v4f acc[NI][NJ];
@@ -591,16 +591,19 @@ __global__ void __launch_bounds__(256, 2) k_gemm_dma(GemmArgs a) {
 #pragma unroll
       for (int j = 0; j < NJ; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
     auto multiply = [&]() {
-      E8 fi[NI], fj[NJ];
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) fj[j] = OB::frag(lds + out + OA::BYTES, 0, wj + 16 * j, 0);
+      for (int s = 0; s < BK / 32; ++s) {
+        E8 fi[NI], fj[NJ];
 #pragma unroll
-      for (int i = 0; i < NI; ++i) fi[i] = OA::frag(lds + out, 0, wi + 16 * i, 0);
+        for (int j = 0; j < NJ; ++j) fj[j] = OB::frag(lds + out + OA::BYTES, 0, wj + 16 * j, s);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) fi[i] = OA::frag(lds + out, 0, wi + 16 * i, s);
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) acc[i][j] = mma(fj[j], fi[i], acc[i][j]);
+      }
       next(out);
-#pragma unroll
-      for (int i = 0; i < NI; ++i)
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) acc[i][j] = mma(fj[j], fi[i], acc[i][j]);
     };
     const int64_t nk = (k1 - k0 + BK - 1) / BK;
     int64_t n = 0;
@@ -804,41 +807,47 @@ static bool aligned(const void *p, int64_t ld, size_t e, size_t to) {
 // cheapest by an estimate of its time in us, from what was measured on MI355X: a
 // block takes its tile's products at `rate` / 256 (TFLOP/s) where blocks share a
 // CU, at `alone` / 256 where it has one to itself, but at least `step` for each
-// K-tile of bk; parts cost a launch, and their sums' way through memory.
+// K-tile of bk, and all of them together the operands' bytes at `stream` TB/s;
+// parts cost a launch, and their sums' way through memory.
 // @@
+enum { PROD_Y, PROD_DX, PROD_DW };
 struct Split {
   int side, parts;
   int64_t kchunk;
 };
-static Split split_of(int64_t I, int J, int64_t K, int dtype, bool both_transposed) {
+static Split split_of(int64_t I, int J, int64_t K, int dtype, int prod) {
   struct Kind {
     int side, ti, tj, bk;
-    double rate, alone, step;
+    double rate, alone, step, stream;
   };
-  const bool f32 = dtype == NR_F32;
-  const double small = both_transposed ? 280 : 390;
-  const Kind kinds[3] = {
-      f32 ? Kind{64, 64, 64, 64, 130, 105, 1.6} : Kind{64, 64, 64, 128, small, 0.8 * small, 1.5},
-      f32 ? Kind{128, 128, 128, 32, 190, 110, 1.8} : Kind{128, 128, 128, 32, 850, 800, 0.35},
-      Kind{256, 256, 128, 32, 1000, 800, 0.45}};
+  const double small = prod == PROD_DW ? 280 : 390;
+  static constexpr Kind f32[2] = {{64, 64, 64, 64, 130, 105, 1.6, 2.9},
+                                  {128, 128, 128, 32, 190, 110, 1.8, 2.9}};
+  // (256 x 128 only where an operand is read along its side: 32 of k of a row that
+  // runs along k are half a line)
+  const Kind h16[3] = {{256, 256, 128, 32, 1000, 830, 0.45, 4.0},
+                       {128, 128, 128, 64, 950, 850, 0.85, 4.0},
+                       {64, 64, 64, 128, small, 0.8 * small, 1.5, 2.9}};
+  const Kind *kind = dtype == NR_F32 ? f32 : prod == PROD_Y ? h16 + 1 : h16;
+  const int kinds = dtype == NR_F32 || prod == PROD_Y ? 2 : 3;
+  const double mbytes = 1e-6 * (dtype == NR_F32 ? 4 : 2) * ((double)I + J) * (double)K;
   Split best{64, 1, 128};
-  double least = 0.0;
-  for (int q = 0; q < (f32 ? 2 : 3); ++q) {
-    const Kind &kind = kinds[q];
-    const double tiles = (double)(up(I, kind.ti) / kind.ti) * (double)(up(J, kind.tj) / kind.tj);
+  double least = INFINITY;
+  for (int q = 0; q < kinds; ++q, ++kind) {
+    const double tiles = (double)(up(I, kind->ti) / kind->ti) * (double)(up(J, kind->tj) / kind->tj);
     for (int want = 1; want <= 256; want *= 2) {
       if (want > 1 && (K < 256 * want || tiles * want > 2048)) break;
       const int64_t kc = K > 0 ? up((K + want - 1) / want, 128) : 128;
       const int parts = K > 0 ? (int)((K + kc - 1) / kc) : 1;
-      const double block = 2e-6 * 256 * kind.ti * kind.tj * kc;
+      const double block = 2e-6 * 256 * kind->ti * kind->tj * kc;
       const int64_t per_cu = (int64_t)((tiles * parts + 255) / 256);
-      const double busy = per_cu / 2 * 2 * block / kind.rate + per_cu % 2 * block / kind.alone;
-      const double wait = (per_cu + 1) / 2 * kind.step * (double)((kc + kind.bk - 1) / kind.bk);
-      const double us = (busy > wait ? busy : wait) +
+      const double busy = per_cu / 2 * 2 * block / kind->rate + per_cu % 2 * block / kind->alone;
+      const double wait = (per_cu + 1) / 2 * kind->step * (double)((kc + kind->bk - 1) / kind->bk);
+      const double us = std::fmax(std::fmax(busy, wait), mbytes / kind->stream) +
                         (parts > 1 ? 5.0 + 1.25e-6 * parts * (double)I * J : 0.0);
-      if ((q == 0 && want == 1) || us < least) {
+      if (us < least) {
         least = us;
-        best = Split{kind.side, parts, kc};
+        best = Split{kind->side, parts, kc};
       }
     }
   }
@@ -856,8 +865,8 @@ static Split split_of(int64_t I, int J, int64_t K, int dtype, bool both_transpos
 #endif
   return best;
 }
-static size_t part_bytes(int64_t I, int J, int64_t K, int dtype, bool both_transposed) {
-  const Split sp = split_of(I, J, K, dtype, both_transposed);
+static size_t part_bytes(int64_t I, int J, int64_t K, int dtype, int prod) {
+  const Split sp = split_of(I, J, K, dtype, prod);
   return sp.parts > 1 ? up(sizeof(float) * (size_t)sp.parts * I * up(J, 32), 256) : 0;
 }
 
@@ -891,8 +900,8 @@ static int64_t tile_grid(const GemmArgs &a, int ti, int tj) {
 
 // a product's parts and their place; returns the tile's side
 template <class T>
-static int place(GemmArgs &a, float *ws, bool both_transposed) {
-  const Split sp = split_of(a.I, a.J, a.K, type_of<T>(), both_transposed);
+static int place(GemmArgs &a, float *ws, int prod) {
+  const Split sp = split_of(a.I, a.J, a.K, type_of<T>(), prod);
   a.kchunk = sp.kchunk;
   a.parts = sp.parts;
   a.part = sp.parts > 1 ? ws : nullptr;
@@ -927,10 +936,13 @@ static void gemm(GemmArgs &a, int side, hipStream_t s) {
       const int64_t n = tile_grid(a, side, 128);
       a.grid = n < 512 ? n : 512;   // two blocks a CU
       const dim3 g((unsigned)a.grid);
-      if (side == 256)
-        hipLaunchKernelGGL((k_gemm_dma<T, 256, 128, IK, JK, LIN>), g, dim3(256), 0, s, a);
-      else
-        hipLaunchKernelGGL((k_gemm_dma<T, 128, 128, IK, JK, LIN>), g, dim3(256), 0, s, a);
+      if constexpr (!JK) {
+        if (side == 256) {
+          hipLaunchKernelGGL((k_gemm_dma<T, 256, 128, 32, 3, IK, JK, LIN>), g, dim3(256), 0, s, a);
+          return;
+        }
+      }
+      hipLaunchKernelGGL((k_gemm_dma<T, 128, 128, 64, 2, IK, JK, LIN>), g, dim3(256), 0, s, a);
       return;
     }
   }
@@ -947,7 +959,7 @@ struct LinearPlan {
 static LinearPlan linear_plan(const LinearArgs &a, int dtype) {
   LinearPlan p{};
   p.ldk = up(a.k, 32);
-  const Split sp = split_of(a.m, a.n, a.k, dtype, false);
+  const Split sp = split_of(a.m, a.n, a.k, dtype, PROD_Y);
   // both operands have k along their rows: either's boundaries spoil the product
   p.copy = copy_pays(dtype, a.m, a.k, a.ldx | a.ldw, a.n, sp.side, 768);
   size_t off = 0;
@@ -955,7 +967,7 @@ static LinearPlan linear_plan(const LinearArgs &a, int dtype) {
   p.at_w = off;
   if (p.copy) off += up((size_t)a.n * p.ldk * 2, 256);
   p.at_part = off;
-  p.bytes = off + part_bytes(a.m, a.n, a.k, dtype, false);
+  p.bytes = off + part_bytes(a.m, a.n, a.k, dtype, PROD_Y);
   return p;
 }
 
@@ -982,7 +994,7 @@ static hipError_t linear_t(const LinearArgs &l, int dtype, char *ws, hipStream_t
     if (!direct(a.B, l.k)) a.B = padded<T>(l.w, l.ldw, l.n, l.k, ws + p.at_w, s);
   }
   a.lin = l;
-  gemm<T, true, true, true>(a, place<T>(a, (float *)(ws + p.at_part), false), s);
+  gemm<T, true, true, true>(a, place<T>(a, (float *)(ws + p.at_part), PROD_Y), s);
   if (a.parts > 1)
     hipLaunchKernelGGL(k_linear_join<T>, dim3((unsigned)join_blocks(a)), dim3(256), 0, s, a);
   return hipGetLastError();
@@ -1005,8 +1017,8 @@ struct GradPlan {
 };
 static GradPlan grad_plan(const LinearGradArgs &a, int dtype) {
   GradPlan p{};
-  const int sx = a.dx ? split_of(a.m, a.k, a.n, dtype, false).side : 0;
-  const int sw = a.dw ? split_of(a.n, a.k, a.m, dtype, true).side : 0;
+  const int sx = a.dx ? split_of(a.m, a.k, a.n, dtype, PROD_DX).side : 0;
+  const int sw = a.dw ? split_of(a.n, a.k, a.m, dtype, PROD_DW).side : 0;
   // dz is written where it is another than dy, or dy's rows are off the boundaries
   p.dz = (a.act != NR_ACT_NONE && (a.dx || a.dw)) ||
          copy_pays(dtype, a.m, a.n, a.lddy, a.k, sx > sw ? sx : sw, 512);
@@ -1034,9 +1046,9 @@ static GradPlan grad_plan(const LinearGradArgs &a, int dtype) {
   p.at_cx = off;
   if (p.copy_x) off += up((size_t)a.m * up(a.k, 32) * 2, 256);
   p.at_x = off;
-  if (a.dx) off += part_bytes(a.m, a.k, a.n, dtype, false);
+  if (a.dx) off += part_bytes(a.m, a.k, a.n, dtype, PROD_DX);
   p.at_w = off;
-  if (a.dw) off += part_bytes(a.n, a.k, a.m, dtype, true);
+  if (a.dw) off += part_bytes(a.n, a.k, a.m, dtype, PROD_DW);
   p.bytes = off;
   return p;
 }
@@ -1062,8 +1074,8 @@ static hipError_t linear_grad_t(const LinearGradArgs &l, int dtype, char *ws, hi
   w.A = z, w.B = l.x;
   w.out = l.dw, w.ldo = l.lddw;
   const bool dx = l.dx && l.m > 0, dw = l.dw;
-  const int sx = dx ? place<T>(x, (float *)(ws + p.at_x), false) : 0;
-  const int sw = dw ? place<T>(w, (float *)(ws + p.at_w), true) : 0;
+  const int sx = dx ? place<T>(x, (float *)(ws + p.at_x), PROD_DX) : 0;
+  const int sw = dw ? place<T>(w, (float *)(ws + p.at_w), PROD_DW) : 0;
   if (p.copy_w && l.m > 0 && !direct(x.B, l.k))
     x.B = padded<T>(l.w, l.ldw, l.n, l.k, ws + p.at_cw, s);
   if (p.copy_x && l.x.hold) {
