@@ -808,14 +808,19 @@ static bool aligned(const void *p, int64_t ld, size_t e, size_t to) {
 // block takes its tile's products at `rate` / 256 (TFLOP/s) where blocks share a
 // CU, at `alone` / 256 where it has one to itself, but at least `step` for each
 // K-tile of bk, and all of them together the operands' bytes at `stream` TB/s;
-// parts cost a launch, and their sums' way through memory.
-// @@
+// parts cost a launch, and their sums' way through memory.  Measured, us, the
+// chosen one last: y of 10,000 x 1536 -> 512 fp32 in 128 x 128 168, 64 x 64 137, 128 x
+// 128 in four parts 124; bf16 700 x 2000 -> 900 64 x 64 39, 128 x 128 26, in four parts
+// 19; 4096 x 512 -> 512 128 x 128 13, 64 x 64 9.8; 48 x 4096 -> 4096 64 x 64 in eight
+// parts 20, 128 x 128 in eight 15.6; 16,384 x 512 -> 512 64 x 64 24, 128 x 128 17.5; dx of
+// 65,536 x 4096 -> 1024 128 x 128 608, 256 x 128 560; dw of 65,536 rows, 4096 x 1024, 128 x
+// 128 in two parts 517, 256 x 128 in four 501
 enum { PROD_Y, PROD_DX, PROD_DW };
 struct Split {
   int side, parts;
   int64_t kchunk;
 };
-static Split split_of(int64_t I, int J, int64_t K, int dtype, int prod) {
+static Split split_of(int64_t I, int J, int64_t K, int dtype, int prod, bool large = true) {
   struct Kind {
     int side, ti, tj, bk;
     double rate, alone, step, stream;
@@ -828,8 +833,10 @@ static Split split_of(int64_t I, int J, int64_t K, int dtype, int prod) {
   const Kind h16[3] = {{256, 256, 128, 32, 1000, 830, 0.45, 4.0},
                        {128, 128, 128, 64, 950, 850, 0.85, 4.0},
                        {64, 64, 64, 128, small, 0.8 * small, 1.5, 2.9}};
-  const Kind *kind = dtype == NR_F32 ? f32 : prod == PROD_Y ? h16 + 1 : h16;
-  const int kinds = dtype == NR_F32 || prod == PROD_Y ? 2 : 3;
+  // !large: 16-bit operands that cannot go straight into LDS
+  const int skip = !large ? 2 : prod == PROD_Y ? 1 : 0;
+  const Kind *kind = dtype == NR_F32 ? f32 : h16 + skip;
+  const int kinds = dtype == NR_F32 ? 2 : 3 - skip;
   const double mbytes = 1e-6 * (dtype == NR_F32 ? 4 : 2) * ((double)I + J) * (double)K;
   Split best{64, 1, 128};
   double least = INFINITY;
@@ -851,28 +858,10 @@ static Split split_of(int64_t I, int J, int64_t K, int dtype, int prod) {
       }
     }
   }
-#ifdef NR_EXPERIMENT
-  int64_t parts = best.parts;
-  if (const char *f = getenv("NR_SIDE")) best.side = atoi(f);
-  if (const char *f = getenv("NR_PARTS")) {
-    parts = atoi(f);
-    const int64_t most = K / 256 < 64 ? K / 256 : 64;
-    if (parts > most) parts = most;
-    if (parts < 2) parts = 1;
-    best.kchunk = K > 0 ? up((K + parts - 1) / parts, 128) : 128;
-    best.parts = K > 0 ? (int)((K + best.kchunk - 1) / best.kchunk) : 1;
-  }
-#endif
   return best;
 }
-static size_t part_bytes(int64_t I, int J, int64_t K, int dtype, int prod) {
-  const Split sp = split_of(I, J, K, dtype, prod);
+static size_t part_bytes(const Split &sp, int64_t I, int J) {
   return sp.parts > 1 ? up(sizeof(float) * (size_t)sp.parts * I * up(J, 32), 256) : 0;
-}
-
-template <class T>
-static constexpr int type_of() {
-  return sizeof(T) == 4 ? NR_F32 : __is_same(T, bf16_t) ? NR_BF16 : NR_F16;
 }
 
 // an operand that can go straight into LDS: whole chunks (or zeros up to the row
@@ -884,29 +873,24 @@ static bool direct(const LayerMat &m, int64_t width) {
 
 // Rows that lie off the 16-byte boundaries can be read, but not straight into LDS,
 // and a load across two lines costs two: us of bf16 products at widths of 1024 /
-// 1023, 16,384 rows: y 50 / 73, dx 38 / 94, dw 61 / 111.  A copy with padded rows
-// (k_pad_rows, 4 bytes of traffic an element at some 5 TB/s and a launch) pays
-// where an element goes into enough products: `products` per element of it
-static bool copy_pays(int dtype, int64_t rows, int64_t width, int64_t ld, int64_t products,
-                      int side, int64_t from) {
-  return dtype != NR_F32 && side >= 128 && (width % 8 != 0 || ld % 8 != 0) && rows > 0 &&
-         products >= from;
-}
+// 1023, 16,384 rows: y 50 / 73, dx 38 / 94, dw 61 / 111.  So 16-bit operands of large
+// tiles are copied to padded rows first (k_pad_rows: 4 bytes of traffic an element
+// at some 5 TB/s, and a launch) where an element goes into at least COPY_FROM
+// products: y of 65,536 x 1001 -> 301 112 with the copy, 145 without; dw of 16,384 x
+// 333 -> 300 33 and 35.  The rest go in 64 x 64 tiles by way of registers
+constexpr int COPY_FROM = 256;
+static bool off_lines(int64_t width, int64_t ld) { return width % 8 != 0 || ld % 8 != 0; }
 
 static int64_t tile_grid(const GemmArgs &a, int ti, int tj) {
   const int64_t n = up(up(a.I, ti) / ti * (up(a.J, tj) / tj) * a.parts, 8);
   return n < 1 << 20 ? n : 1 << 20;   // blocks take further tiles in turn
 }
 
-// a product's parts and their place; returns the tile's side
-template <class T>
-static int place(GemmArgs &a, float *ws, int prod) {
-  const Split sp = split_of(a.I, a.J, a.K, type_of<T>(), prod);
+static void place(GemmArgs &a, const Split &sp, void *ws) {
   a.kchunk = sp.kchunk;
   a.parts = sp.parts;
-  a.part = sp.parts > 1 ? ws : nullptr;
+  a.part = sp.parts > 1 ? (float *)ws : nullptr;
   a.ldp = up(a.J, 32);
-  return sp.side;
 }
 static int64_t join_blocks(const GemmArgs &a) {
   if (a.parts < 2) return 0;
@@ -946,28 +930,35 @@ static void gemm(GemmArgs &a, int side, hipStream_t s) {
       return;
     }
   }
-  if (side == 64) gemm_reg<T, 64, IK, JK, LIN>(a, s);
-  else gemm_reg<T, 128, IK, JK, LIN>(a, s);
+  if constexpr (sizeof(T) == 4) {
+    if (side == 128) {
+      gemm_reg<T, 128, IK, JK, LIN>(a, s);
+      return;
+    }
+  }
+  gemm_reg<T, 64, IK, JK, LIN>(a, s);
 }
 
 // Work space of the forward pass: copies of x and w with padded rows, and the parts
 struct LinearPlan {
+  Split sp;
   bool copy;
-  int64_t ldk;
   size_t at_w, at_part, bytes;
 };
 static LinearPlan linear_plan(const LinearArgs &a, int dtype) {
   LinearPlan p{};
-  p.ldk = up(a.k, 32);
-  const Split sp = split_of(a.m, a.n, a.k, dtype, PROD_Y);
-  // both operands have k along their rows: either's boundaries spoil the product
-  p.copy = copy_pays(dtype, a.m, a.k, a.ldx | a.ldw, a.n, sp.side, 768);
+  p.sp = split_of(a.m, a.n, a.k, dtype, PROD_Y);
+  if (dtype != NR_F32 && p.sp.side >= 128 && off_lines(a.k, a.ldx | a.ldw)) {
+    p.copy = a.m > 0 && a.n >= COPY_FROM;
+    if (!p.copy) p.sp = split_of(a.m, a.n, a.k, dtype, PROD_Y, false);
+  }
+  const int64_t ldk = up(a.k, 32);
   size_t off = 0;
-  if (p.copy) off += up((size_t)a.m * p.ldk * 2, 256);
+  if (p.copy) off += up((size_t)a.m * ldk * 2, 256);
   p.at_w = off;
-  if (p.copy) off += up((size_t)a.n * p.ldk * 2, 256);
+  if (p.copy) off += up((size_t)a.n * ldk * 2, 256);
   p.at_part = off;
-  p.bytes = off + part_bytes(a.m, a.n, a.k, dtype, PROD_Y);
+  p.bytes = off + part_bytes(p.sp, a.m, a.n);
   return p;
 }
 
@@ -994,7 +985,8 @@ static hipError_t linear_t(const LinearArgs &l, int dtype, char *ws, hipStream_t
     if (!direct(a.B, l.k)) a.B = padded<T>(l.w, l.ldw, l.n, l.k, ws + p.at_w, s);
   }
   a.lin = l;
-  gemm<T, true, true, true>(a, place<T>(a, (float *)(ws + p.at_part), PROD_Y), s);
+  place(a, p.sp, ws + p.at_part);
+  gemm<T, true, true, true>(a, p.sp.side, s);
   if (a.parts > 1)
     hipLaunchKernelGGL(k_linear_join<T>, dim3((unsigned)join_blocks(a)), dim3(256), 0, s, a);
   return hipGetLastError();
@@ -1009,6 +1001,7 @@ hipError_t launch_linear(const LinearArgs &a, int dtype, void *ws, hipStream_t s
 // Work space of the gradients: dz, the column sums of its blocks, copies of w and x
 // with padded rows, and the parts of the two products
 struct GradPlan {
+  Split sx, sw;
   bool act, dz;          // the pass over dy runs; it writes dz
   int64_t rows, nb, ldz; // rows per block of that pass, its blocks, dz's row stride
   int ct;
@@ -1017,14 +1010,22 @@ struct GradPlan {
 };
 static GradPlan grad_plan(const LinearGradArgs &a, int dtype) {
   GradPlan p{};
-  const int sx = a.dx ? split_of(a.m, a.k, a.n, dtype, PROD_DX).side : 0;
-  const int sw = a.dw ? split_of(a.n, a.k, a.m, dtype, PROD_DW).side : 0;
-  // dz is written where it is another than dy, or dy's rows are off the boundaries
+  // dz is written where it is another than dy, and as a padded copy of dy; w is
+  // copied for dx, x (or what is held of it) for dw
+  if (a.dx) p.sx = split_of(a.m, a.k, a.n, dtype, PROD_DX);
+  if (a.dw) p.sw = split_of(a.n, a.k, a.m, dtype, PROD_DW);
+  const bool h16 = dtype != NR_F32 && a.m > 0;
+  const bool big_x = h16 && a.dx && p.sx.side >= 128, big_w = h16 && a.dw && p.sw.side >= 128;
   p.dz = (a.act != NR_ACT_NONE && (a.dx || a.dw)) ||
-         copy_pays(dtype, a.m, a.n, a.lddy, a.k, sx > sw ? sx : sw, 512);
-  p.copy_w = a.dx && copy_pays(dtype, a.n, a.k, a.ldw, a.m, sx, 512);
-  p.copy_x = a.dw && (a.x.hold ? dtype != NR_F32 && sw >= 128 && a.m > 0 && a.n >= 512
-                               : copy_pays(dtype, a.m, a.k, a.x.ld, a.n, sw, 512));
+         ((big_x || big_w) && off_lines(a.n, a.lddy) && a.k >= COPY_FROM);
+  const bool z_off = !p.dz && off_lines(a.n, a.lddy);
+  const bool w_off = off_lines(a.k, a.ldw), x_off = a.x.hold || off_lines(a.k, a.x.ld);
+  p.copy_w = big_x && !z_off && w_off && a.m >= COPY_FROM;
+  p.copy_x = big_w && !z_off && x_off && a.n >= COPY_FROM;
+  if (big_x && (z_off || (w_off && !p.copy_w)))
+    p.sx = split_of(a.m, a.k, a.n, dtype, PROD_DX, false);
+  if (big_w && (z_off || (x_off && !p.copy_x)))
+    p.sw = split_of(a.n, a.k, a.m, dtype, PROD_DW, false);
   p.act = p.dz || a.db;
   p.ct = 4;   // whole groups of 32 columns
   while (p.ct < 256 && p.ct * 8 < a.n) p.ct *= 2;
@@ -1046,9 +1047,9 @@ static GradPlan grad_plan(const LinearGradArgs &a, int dtype) {
   p.at_cx = off;
   if (p.copy_x) off += up((size_t)a.m * up(a.k, 32) * 2, 256);
   p.at_x = off;
-  if (a.dx) off += part_bytes(a.m, a.k, a.n, dtype, PROD_DX);
+  if (a.dx) off += part_bytes(p.sx, a.m, a.k);
   p.at_w = off;
-  if (a.dw) off += part_bytes(a.n, a.k, a.m, dtype, PROD_DW);
+  if (a.dw) off += part_bytes(p.sw, a.n, a.k);
   p.bytes = off;
   return p;
 }
@@ -1074,9 +1075,9 @@ static hipError_t linear_grad_t(const LinearGradArgs &l, int dtype, char *ws, hi
   w.A = z, w.B = l.x;
   w.out = l.dw, w.ldo = l.lddw;
   const bool dx = l.dx && l.m > 0, dw = l.dw;
-  const int sx = dx ? place<T>(x, (float *)(ws + p.at_x), PROD_DX) : 0;
-  const int sw = dw ? place<T>(w, (float *)(ws + p.at_w), PROD_DW) : 0;
-  if (p.copy_w && l.m > 0 && !direct(x.B, l.k))
+  if (dx) place(x, p.sx, ws + p.at_x);
+  if (dw) place(w, p.sw, ws + p.at_w);
+  if (p.copy_w && !direct(x.B, l.k))
     x.B = padded<T>(l.w, l.ldw, l.n, l.k, ws + p.at_cw, s);
   if (p.copy_x && l.x.hold) {
     const int64_t ld = up(l.k, 32);   // its padding is zeros
@@ -1084,17 +1085,17 @@ static hipError_t linear_grad_t(const LinearGradArgs &l, int dtype, char *ws, hi
                                      dtype, ws + p.at_cx, ld, s);
     if (e != hipSuccess) return e;
     w.B = LayerMat{ws + p.at_cx, ld, 0, nullptr, true};
-  } else if (p.copy_x && l.m > 0 && !direct(w.B, l.k)) {
+  } else if (p.copy_x && !direct(w.B, l.k)) {
     w.B = padded<T>(l.x.p, l.x.ld, l.m, l.k, ws + p.at_cx, s);
   }
-  if (sx == 64 && sw == 64) {
+  if (dx && dw && p.sx.side == 64 && p.sw.side == 64) {
     x.grid = tile_grid(x, 64, 64), w.grid = tile_grid(w, 64, 64);
     const dim3 g((unsigned)(x.grid + w.grid));
     if (w.B.hold) hipLaunchKernelGGL((k_gemm_two<T, true>), g, dim3(256), 0, s, x, w);
     else hipLaunchKernelGGL((k_gemm_two<T, false>), g, dim3(256), 0, s, x, w);
   } else {
-    if (dx) gemm<T, true, false, false>(x, sx, s);
-    if (dw) gemm<T, false, false, false>(w, sw, s);
+    if (dx) gemm<T, true, false, false>(x, p.sx.side, s);
+    if (dw) gemm<T, false, false, false>(w, p.sw.side, s);
   }
   const int64_t bx = dx ? join_blocks(x) : 0, bw = dw ? join_blocks(w) : 0;
   const int64_t bc = l.db ? (l.n + 15) / 16 : 0;
