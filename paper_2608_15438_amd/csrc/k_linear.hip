@@ -819,6 +819,7 @@ enum { PROD_Y, PROD_DX, PROD_DW };
 struct Split {
   int side, parts;
   int64_t kchunk;
+  double us;   // the estimate, without a launch's fixed time
 };
 static Split split_of(int64_t I, int J, int64_t K, int dtype, int prod, bool large = true) {
   struct Kind {
@@ -838,8 +839,7 @@ static Split split_of(int64_t I, int J, int64_t K, int dtype, int prod, bool lar
   const Kind *kind = dtype == NR_F32 ? f32 : h16 + skip;
   const int kinds = dtype == NR_F32 ? 2 : 3 - skip;
   const double mbytes = 1e-6 * (dtype == NR_F32 ? 4 : 2) * ((double)I + J) * (double)K;
-  Split best{64, 1, 128};
-  double least = INFINITY;
+  Split best{64, 1, 128, INFINITY};
   for (int q = 0; q < kinds; ++q, ++kind) {
     const double tiles = (double)(up(I, kind->ti) / kind->ti) * (double)(up(J, kind->tj) / kind->tj);
     for (int want = 1; want <= 256; want *= 2) {
@@ -852,10 +852,7 @@ static Split split_of(int64_t I, int J, int64_t K, int dtype, int prod, bool lar
       const double wait = (per_cu + 1) / 2 * kind->step * (double)((kc + kind->bk - 1) / kind->bk);
       const double us = std::fmax(std::fmax(busy, wait), mbytes / kind->stream) +
                         (parts > 1 ? 5.0 + 1.25e-6 * parts * (double)I * J : 0.0);
-      if (us < least) {
-        least = us;
-        best = Split{kind->side, parts, kc};
-      }
+      if (us < best.us) best = Split{kind->side, parts, kc, us};
     }
   }
   return best;
@@ -873,13 +870,15 @@ static bool direct(const LayerMat &m, int64_t width) {
 
 // Rows that lie off the 16-byte boundaries can be read, but not straight into LDS,
 // and a load across two lines costs two: us of bf16 products at widths of 1024 /
-// 1023, 16,384 rows: y 50 / 73, dx 38 / 94, dw 61 / 111.  So 16-bit operands of large
-// tiles are copied to padded rows first (k_pad_rows: 4 bytes of traffic an element
-// at some 5 TB/s, and a launch) where an element goes into at least COPY_FROM
-// products: y of 65,536 x 1001 -> 301 112 with the copy, 145 without; dw of 16,384 x
-// 333 -> 300 33 and 35.  The rest go in 64 x 64 tiles by way of registers
-constexpr int COPY_FROM = 256;
+// 1023, 16,384 rows: y 50 / 73, dx 38 / 94, dw 61 / 111.  So 16-bit operands are
+// copied to padded rows first (k_pad_rows: 4 us, and 4 bytes an element at some 5
+// TB/s) where large tiles with the copies are estimated to be faster than small
+// ones by way of registers, which take a third longer for such rows: y of 65,536 x
+// 1001 -> 301 112 us with copies, 145 without; dw of 16,384 x 333 -> 300 33 and 35
 static bool off_lines(int64_t width, int64_t ld) { return width % 8 != 0 || ld % 8 != 0; }
+static bool copies_pay(const Split &large, const Split &small, int copies, int64_t elements) {
+  return large.us + 4.0 * copies + 8e-7 * (double)elements < 1.33 * small.us;
+}
 
 static int64_t tile_grid(const GemmArgs &a, int ti, int tj) {
   const int64_t n = up(up(a.I, ti) / ti * (up(a.J, tj) / tj) * a.parts, 8);
@@ -949,8 +948,9 @@ static LinearPlan linear_plan(const LinearArgs &a, int dtype) {
   LinearPlan p{};
   p.sp = split_of(a.m, a.n, a.k, dtype, PROD_Y);
   if (dtype != NR_F32 && p.sp.side >= 128 && off_lines(a.k, a.ldx | a.ldw)) {
-    p.copy = a.m > 0 && a.n >= COPY_FROM;
-    if (!p.copy) p.sp = split_of(a.m, a.n, a.k, dtype, PROD_Y, false);
+    const Split small = split_of(a.m, a.n, a.k, dtype, PROD_Y, false);
+    p.copy = a.m > 0 && copies_pay(p.sp, small, 2, (a.m + a.n) * a.k);
+    if (!p.copy) p.sp = small;
   }
   const int64_t ldk = up(a.k, 32);
   size_t off = 0;
@@ -1014,18 +1014,23 @@ static GradPlan grad_plan(const LinearGradArgs &a, int dtype) {
   // copied for dx, x (or what is held of it) for dw
   if (a.dx) p.sx = split_of(a.m, a.k, a.n, dtype, PROD_DX);
   if (a.dw) p.sw = split_of(a.n, a.k, a.m, dtype, PROD_DW);
+  p.dz = a.act != NR_ACT_NONE && (a.dx || a.dw);
   const bool h16 = dtype != NR_F32 && a.m > 0;
-  const bool big_x = h16 && a.dx && p.sx.side >= 128, big_w = h16 && a.dw && p.sw.side >= 128;
-  p.dz = (a.act != NR_ACT_NONE && (a.dx || a.dw)) ||
-         ((big_x || big_w) && off_lines(a.n, a.lddy) && a.k >= COPY_FROM);
   const bool z_off = !p.dz && off_lines(a.n, a.lddy);
+  auto choose = [&](Split &sp, int64_t I, int J, int64_t K, int prod, bool off, int64_t elements) {
+    if (!h16 || sp.side < 128 || !(z_off || off)) return false;
+    const Split small = split_of(I, J, K, dtype, prod, false);
+    if (copies_pay(sp, small, z_off + off, (z_off ? a.m * a.n : 0) + (off ? elements : 0)))
+      return true;
+    sp = small;
+    return false;
+  };
   const bool w_off = off_lines(a.k, a.ldw), x_off = a.x.hold || off_lines(a.k, a.x.ld);
-  p.copy_w = big_x && !z_off && w_off && a.m >= COPY_FROM;
-  p.copy_x = big_w && !z_off && x_off && a.n >= COPY_FROM;
-  if (big_x && (z_off || (w_off && !p.copy_w)))
-    p.sx = split_of(a.m, a.k, a.n, dtype, PROD_DX, false);
-  if (big_w && (z_off || (x_off && !p.copy_x)))
-    p.sw = split_of(a.n, a.k, a.m, dtype, PROD_DW, false);
+  const bool cx = a.dx && choose(p.sx, a.m, a.k, a.n, PROD_DX, w_off, (int64_t)a.n * a.k);
+  const bool cw = a.dw && choose(p.sw, a.n, a.k, a.m, PROD_DW, x_off, a.m * a.k);
+  p.copy_w = cx && w_off;
+  p.copy_x = cw && x_off;
+  if (z_off && (cx || cw)) p.dz = true;
   p.act = p.dz || a.db;
   p.ct = 4;   // whole groups of 32 columns
   while (p.ct < 256 && p.ct * 8 < a.n) p.ct *= 2;
