@@ -728,15 +728,16 @@ __global__ void __launch_bounds__(256) k_grad_join(GemmArgs x, GemmArgs w, int64
   }
 }
 
+constexpr int ACT_THREADS = 512;
 // dz = dy act'(pre) of `rows` rows per block, rounded to the type, zeros from n up to
-// ldz (a multiple of 32; dz NULL: not wanted), and its column sums over them (part NULL: not wanted).  The 256
-// threads are 256 / ct rows of ct threads, eight columns each
+// ldz (a multiple of 32; dz NULL: not wanted), and its column sums over them (part NULL: not wanted).  The 512
+// threads are 512 / ct rows of ct threads, eight columns each
 template <class T>
-__global__ void __launch_bounds__(256) k_act_grad(LinearGradArgs a, int64_t rows, int ct, T *dz,
+__global__ void __launch_bounds__(ACT_THREADS) k_act_grad(LinearGradArgs a, int64_t rows, int ct, T *dz,
                                                   int64_t ldz, float *part) {
-  __shared__ float red[256][9];
+  __shared__ float red[ACT_THREADS][9];
   constexpr bool exact = sizeof(T) == 4;
-  const int tc = threadIdx.x % ct, tr = threadIdx.x / ct, rt = 256 / ct;
+  const int tc = threadIdx.x % ct, tr = threadIdx.x / ct, rt = ACT_THREADS / ct;
   const int c0 = (blockIdx.y * ct + tc) * 8;
   const int64_t r0 = (int64_t)blockIdx.x * rows, r1 = r0 + rows < a.m ? r0 + rows : a.m;
   float s[8] = {};
@@ -1035,7 +1036,7 @@ static GradPlan grad_plan(const LinearGradArgs &a, int dtype) {
   p.ct = 4;   // whole groups of 32 columns
   while (p.ct < 256 && p.ct * 8 < a.n) p.ct *= 2;
   // blocks of the pass: some thousand in all, at most 512 of them along the rows
-  const int64_t rt = 256 / p.ct, across = (a.n + 8 * p.ct - 1) / (8 * p.ct);
+  const int64_t rt = ACT_THREADS / p.ct, across = (a.n + 8 * p.ct - 1) / (8 * p.ct);
   int64_t blocks = 1024 / across;
   blocks = blocks > 512 ? 512 : blocks;
   p.rows = up((a.m + blocks - 1) / blocks, 4 * rt);
@@ -1068,7 +1069,7 @@ static hipError_t linear_grad_t(const LinearGradArgs &l, int dtype, char *ws, hi
   float *cols = l.db ? (float *)(ws + p.at_cols) : nullptr;
   if (p.act && l.m > 0) {
     const dim3 g((unsigned)p.nb, (l.n + 8 * p.ct - 1) / (8 * p.ct));
-    hipLaunchKernelGGL(k_act_grad<T>, g, dim3(256), 0, s, l, p.rows, p.ct, dz, p.ldz, cols);
+    hipLaunchKernelGGL(k_act_grad<T>, g, dim3(ACT_THREADS), 0, s, l, p.rows, p.ct, dz, p.ldz, cols);
   }
   const LayerMat z = p.dz ? LayerMat{dz, p.ldz, 0, nullptr, true}
                           : LayerMat{l.dy, l.lddy, 0, nullptr, false};
