@@ -45,15 +45,16 @@ static unsigned hold_grid(int64_t m, int d) {
 template <class T>
 static hipError_t hold_t(const void *x, int64_t ldx, int64_t m, int d, int hold, uint8_t *q,
                          uint8_t *scale, hipStream_t s) {
-  hipLaunchKernelGGL(k_act_hold<T>, dim3(hold_grid(m, d)), dim3(256), 0, s, (const T *)x, ldx, m, d, hold, q,
-                     scale);
+  hipLaunchKernelGGL(k_act_hold<T>, dim3(hold_grid(m, d)), dim3(256), 0, s, (const T *)x, ldx, m,
+                     d, hold, q, scale);
   return hipGetLastError();
 }
 
 template <class T>
 static hipError_t read_t(const uint8_t *q, const uint8_t *scale, int64_t m, int d, int hold,
                          void *y, int64_t ldy, hipStream_t s) {
-  hipLaunchKernelGGL(k_act_read<T>, dim3(hold_grid(m, d)), dim3(256), 0, s, q, scale, m, d, hold, (T *)y, ldy);
+  hipLaunchKernelGGL(k_act_read<T>, dim3(hold_grid(m, d)), dim3(256), 0, s, q, scale, m, d, hold,
+                     (T *)y, ldy);
   return hipGetLastError();
 }
 

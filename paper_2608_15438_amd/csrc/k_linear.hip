@@ -312,6 +312,7 @@ __device__ float plain_chain(const LayerMat &A, const LayerMat &B, int64_t i, in
       w = ((const float *)B.p)[JK ? j * B.ld + k : k * B.ld + j];
     }
     s = fmaf(x, w, s);
+    if (s != s) break;   // no number it stays
   }
   return s;
 }
@@ -730,11 +731,12 @@ __global__ void __launch_bounds__(256) k_grad_join(GemmArgs x, GemmArgs w, int64
 
 constexpr int ACT_THREADS = 512;
 // dz = dy act'(pre) of `rows` rows per block, rounded to the type, zeros from n up to
-// ldz (a multiple of 32; dz NULL: not wanted), and its column sums over them (part NULL: not wanted).  The 512
-// threads are 512 / ct rows of ct threads, eight columns each
+// ldz (a multiple of 32; dz NULL: not wanted), and its column sums over them (part
+// NULL: not wanted).  The threads are ACT_THREADS / ct rows of ct threads, eight
+// columns each
 template <class T>
-__global__ void __launch_bounds__(ACT_THREADS) k_act_grad(LinearGradArgs a, int64_t rows, int ct, T *dz,
-                                                  int64_t ldz, float *part) {
+__global__ void __launch_bounds__(ACT_THREADS) k_act_grad(LinearGradArgs a, int64_t rows, int ct,
+                                                          T *dz, int64_t ldz, float *part) {
   __shared__ float red[ACT_THREADS][9];
   constexpr bool exact = sizeof(T) == 4;
   const int tc = threadIdx.x % ct, tr = threadIdx.x / ct, rt = ACT_THREADS / ct;

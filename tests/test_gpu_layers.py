@@ -141,7 +141,8 @@ def test_linear_grad(m, k, n, t):
 
 @pytest.mark.parametrize("t", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("m,k,n", [(4200, 200, 4104), (200, 4200, 4104), (4200, 4104, 200),
-                                   (4097, 72, 4099), (16_400, 1030, 264), (9000, 520, 48)])
+                                   (4097, 72, 4099), (16_400, 1030, 264), (9000, 520, 48),
+                                   (16_384, 1024, 1024), (300, 40, 8192), (20_000, 33, 100)])
 def test_linear_many_tiles(m, k, n, t):
     # each product with more outputs than the chip takes at once, its ends inside tiles
     g, dt, x, w, b, r = linear_case(m, k, n, t)
@@ -239,6 +240,35 @@ def test_linear_large_values(t):
     y = NR.nr_linear(x, w)
     want = x.double() @ w.double().T
     assert torch.equal(y.double(), want)
+
+
+@pytest.mark.parametrize("t", ["bf16", "f16"])
+@pytest.mark.parametrize("m,k,n", [(5, 70, 66), (300, 512, 512), (4200, 256, 4104)])
+def test_linear_small_values(m, k, n, t):
+    # subnormal elements count as they are
+    g = gen(m, k, n, t, "sub")
+    dt = R.TYPES[t]
+    f = torch.finfo(dt)
+    x = (torch.randint(-200, 200, (m, k), generator=g, device=DEV).double()
+         * (f.smallest_normal * f.eps)).to(dt)
+    w = torch.randn((n, k), generator=g, device=DEV).to(dt) * 64
+    check_linear(x, w, None, None, "none", *NR.nr_linear(x, w, pre=True))
+    dy = rows(g, m, n, dt)
+    dx, dw, db = NR.nr_linear_grad(dy, x, w)
+    grad_check(dy, x, w, "none", None, (dx, dw, db), False)
+
+
+def test_linear_small_values_fp32():
+    # a float's parts are bf16: below 2^-110 the lowest of them are subnormal, and
+    # what they lose is at most 2^-126 for an element
+    g = gen("sub32")
+    for e in (-100, -112, -125, -135):
+        x = torch.randn((70, 96), generator=g, device=DEV) * 2.0 ** e
+        w = torch.randn((40, 96), generator=g, device=DEV)
+        y = NR.nr_linear(x, w)
+        want = x.double() @ w.double().T
+        tol = 98 * U * (x.double().abs() @ w.double().abs().T) + 2.0 ** -126 * w.double().abs().sum(1)
+        close(y, want, tol + R.half_step(want, torch.float32), e)
 
 
 # ---------------------------------------------------------------- 8 bits
