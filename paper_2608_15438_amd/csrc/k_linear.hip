@@ -284,7 +284,8 @@ struct Operand {
     } else {
       typedef __attribute__((address_space(3))) s16x4 lds4;
       const int k = 32 * s + 8 * g + (t >> 2), c = b0 / 8 + ((t & 3) >> 1), in = 8 * (t & 1);
-      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(lds + slot(k, c) * 16 + in));
+      const s16x4 lo =
+          __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(lds + slot(k, c) * 16 + in));
       const s16x4 hi =
           __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(lds + slot(k + 4, c) * 16 + in));
       return __builtin_bit_cast(E8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -517,9 +518,18 @@ __global__ void __launch_bounds__(256, 2) k_gemm_two(GemmArgs x, GemmArgs w) {
 }
 
 // The same for 16-bit operands whose rows lie on 16-byte boundaries: K-tiles go
-// straight from memory into LDS, two ahead of the products.  256 x 128 tiles by
-// four waves: two blocks share a CU, and one reads its operands from LDS, or makes
-// its epilogue, while the other multiplies
+// straight from memory into LDS, NB - 1 of them ahead of the products.  Two blocks
+// of four waves share a CU, and one reads its operands from LDS, or makes its
+// epilogue, while the other multiplies; a block goes on to its next tile with that
+// tile's first K-tiles already under way.  128 x 128 tiles take k 64 at a time, whole
+// lines of rows that run along k (32 at a time the 8192^3 product took 1053 us, 64
+// 945, the library 692 to 708); 256 x 128 tiles, two thirds of the traffic, take 32, for
+// products with an operand that runs along its side (dw of 65,536 rows, 4096 x 1024:
+// 442 us, 1.24 PFLOP/s; in 128 x 128 517).  What bounds it: matrix instructions half
+// of the time, at clocks of 2.0 of 2.4 GHz; the rest are waits for operands.  Tried
+// and slower: one block of eight waves, 256 x 256, operands half a K-tile ahead (1141
+// TFLOP/s at k = 8192, but its epilogue stands alone: 740 us for 65,536 x 1024 ->
+// 4096, now 620); operands from LDS a K-tile ahead with 128 x 128 tiles (1003 / 945 us)
 template <class T, int TI, int TJ, int BK, int NB, bool IK, bool JK, bool LIN>
 __global__ void __launch_bounds__(256, 2) k_gemm_dma(GemmArgs a) {
   constexpr int NI = TI / 32, NJ = TJ / 32;
@@ -592,18 +602,26 @@ __global__ void __launch_bounds__(256, 2) k_gemm_dma(GemmArgs a) {
 #pragma unroll
       for (int j = 0; j < NJ; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
     auto multiply = [&]() {
+      constexpr int H = BK / 32;
+      E8 fi[H][NI], fj[H][NJ];
 #pragma unroll
-      for (int s = 0; s < BK / 32; ++s) {
-        E8 fi[NI], fj[NJ];
+      for (int s = 0; s < H; ++s) {
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) fj[j] = OB::frag(lds + out + OA::BYTES, 0, wj + 16 * j, s);
+        for (int j = 0; j < NJ; ++j) fj[s][j] = OB::frag(lds + out + OA::BYTES, 0, wj + 16 * j, s);
 #pragma unroll
-        for (int i = 0; i < NI; ++i) fi[i] = OA::frag(lds + out, 0, wi + 16 * i, s);
+        for (int i = 0; i < NI; ++i) fi[s][i] = OA::frag(lds + out, 0, wi + 16 * i, s);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      // the wave that multiplies before the other block's: dw of 65,536 rows, 4096 x
+      // 1024, 505 -> 450 us, dx 568 -> 555 (128 x 128 tiles lose 1 %)
+      if constexpr (TI == 256) __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+      for (int s = 0; s < H; ++s)
 #pragma unroll
         for (int i = 0; i < NI; ++i)
 #pragma unroll
-          for (int j = 0; j < NJ; ++j) acc[i][j] = mma(fj[j], fi[i], acc[i][j]);
-      }
+          for (int j = 0; j < NJ; ++j) acc[i][j] = mma(fj[s][j], fi[s][i], acc[i][j]);
+      if constexpr (TI == 256) __builtin_amdgcn_s_setprio(0);
       next(out);
     };
     const int64_t nk = (k1 - k0 + BK - 1) / BK;
@@ -844,7 +862,8 @@ static Split split_of(int64_t I, int J, int64_t K, int dtype, int prod, bool lar
   const double mbytes = 1e-6 * (dtype == NR_F32 ? 4 : 2) * ((double)I + J) * (double)K;
   Split best{64, 1, 128, INFINITY};
   for (int q = 0; q < kinds; ++q, ++kind) {
-    const double tiles = (double)(up(I, kind->ti) / kind->ti) * (double)(up(J, kind->tj) / kind->tj);
+    const double tiles =
+        (double)(up(I, kind->ti) / kind->ti) * (double)(up(J, kind->tj) / kind->tj);
     for (int want = 1; want <= 256; want *= 2) {
       if (want > 1 && (K < 256 * want || tiles * want > 2048)) break;
       const int64_t kc = K > 0 ? up((K + want - 1) / want, 128) : 128;
