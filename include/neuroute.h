@@ -315,13 +315,15 @@ nr_status nr_lsim_grad_at(const float *d2_emb, const float *lat, int64_t B, int3
  * one type: NR_F32, NR_BF16 or NR_F16.  Pointers are aligned to their element;
  * rows that start on 16-byte boundaries are read fastest.  Sums are held in
  * fp32 and rounded to the type once; every result is the same bit for bit on
- * every call with the same inputs.  Outputs must not overlap inputs or one
- * another.  Widths are 1..NR_MAX_WIDTH, rows >= 0 (0 rows: no output rows, and
- * gradients of parameters are zero).  `ws` is DEVICE scratch of at least the
- * bytes that the call's _ws function names for the same description (16-byte
- * aligned; NULL where that is 0), in use until the call's work is done: calls
- * that may overlap in time, and captured graphs that may, need one each.
- * Rows of a batch do not influence one another's outputs. */
+ * every call with the same inputs.  fp32 products are made of bf16 parts, good to
+ * 2^-24 of a product; elements below 2^-110 lose up to 2^-126 of themselves.
+ * Outputs must not overlap inputs or one another.  Widths are 1..NR_MAX_WIDTH,
+ * rows >= 0 (0 rows: no output rows, and gradients of parameters are zero).
+ * `ws` is DEVICE scratch of at least the bytes that the call's _ws function names
+ * for the same description, pointers and strides included (16-byte aligned;
+ * NULL where that is 0), in use until the call's work is done: calls that may
+ * overlap in time, and captured graphs that may, need one each.  Rows of a
+ * batch do not influence one another's outputs. */
 #define NR_MAX_WIDTH 16384
 enum { NR_BF16 = 2, NR_F16 = 3 };   /* further nr_dtype values, for the layers only */
 typedef enum {

@@ -895,11 +895,15 @@ static bool direct(const LayerMat &m, int64_t width) {
 // 1023, 16,384 rows: y 50 / 73, dx 38 / 94, dw 61 / 111.  So 16-bit operands are
 // copied to padded rows first (k_pad_rows: 4 us, and 4 bytes an element at some 5
 // TB/s) where large tiles with the copies are estimated to be faster than small
-// ones by way of registers, which take a third longer for such rows: y of 65,536 x
-// 1001 -> 301 112 us with copies, 145 without; dw of 16,384 x 333 -> 300 33 and 35
+// ones by way of registers, which take half as long again for such rows, and twice
+// as long where they run along the side: us with copies / without, y of 65,536 x
+// 1001 -> 301 112 / 145, 2000 x 1001 -> 2001 31 / 44, its dx 34 / 62, dw 33 / 64; dw of
+// 16,384 x 333 -> 300 33 / 35
 static bool off_lines(int64_t width, int64_t ld) { return width % 8 != 0 || ld % 8 != 0; }
-static bool copies_pay(const Split &large, const Split &small, int copies, int64_t elements) {
-  return large.us + 4.0 * copies + 8e-7 * (double)elements < 1.33 * small.us;
+static bool copies_pay(const Split &large, const Split &small, int prod, int copies,
+                       int64_t elements) {
+  return large.us + 4.0 * copies + 8e-7 * (double)elements <
+         (prod == PROD_Y ? 1.4 : 2.0) * small.us;
 }
 
 static int64_t tile_grid(const GemmArgs &a, int ti, int tj) {
@@ -971,7 +975,7 @@ static LinearPlan linear_plan(const LinearArgs &a, int dtype) {
   p.sp = split_of(a.m, a.n, a.k, dtype, PROD_Y);
   if (dtype != NR_F32 && p.sp.side >= 128 && off_lines(a.k, a.ldx | a.ldw)) {
     const Split small = split_of(a.m, a.n, a.k, dtype, PROD_Y, false);
-    p.copy = a.m > 0 && copies_pay(p.sp, small, 2, (a.m + a.n) * a.k);
+    p.copy = a.m > 0 && copies_pay(p.sp, small, PROD_Y, 2, (a.m + a.n) * a.k);
     if (!p.copy) p.sp = small;
   }
   const int64_t ldk = up(a.k, 32);
@@ -1042,7 +1046,7 @@ static GradPlan grad_plan(const LinearGradArgs &a, int dtype) {
   auto choose = [&](Split &sp, int64_t I, int J, int64_t K, int prod, bool off, int64_t elements) {
     if (!h16 || sp.side < 128 || !(z_off || off)) return false;
     const Split small = split_of(I, J, K, dtype, prod, false);
-    if (copies_pay(sp, small, z_off + off, (z_off ? a.m * a.n : 0) + (off ? elements : 0)))
+    if (copies_pay(sp, small, prod, z_off + off, (z_off ? a.m * a.n : 0) + (off ? elements : 0)))
       return true;
     sp = small;
     return false;
