@@ -315,9 +315,9 @@ nr_status nr_lsim_grad_at(const float *d2_emb, const float *lat, int64_t B, int3
  * one type: NR_F32, NR_BF16 or NR_F16.  Pointers are aligned to their element;
  * rows that start on 16-byte boundaries are read fastest.  Sums are held in
  * fp32 and rounded to the type once; every result is the same bit for bit on
- * every call with the same inputs.  fp32 products are made of bf16 parts, good to
- * 2^-24 of a product; elements below 2^-110 lose up to 2^-126 of themselves.
- * Outputs must not overlap inputs or one another.  Widths are 1..NR_MAX_WIDTH,
+ * every call with the same inputs laid out the same.  fp32 products are made of
+ * bf16 parts, good to 2^-24 of a product; an element below 2^-110 loses up to
+ * 2^-126.  Outputs must not overlap inputs or one another.  Widths are 1..NR_MAX_WIDTH,
  * rows >= 0 (0 rows: no output rows, and gradients of parameters are zero).
  * `ws` is DEVICE scratch of at least the bytes that the call's _ws function names
  * for the same description, pointers and strides included (16-byte aligned;

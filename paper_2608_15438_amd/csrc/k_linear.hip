@@ -78,12 +78,12 @@ __device__ __forceinline__ void finish(const GemmArgs &a, int64_t i, int j, bool
 template <class T>
 struct Tile {
   typedef T E;
-  static constexpr int P = 1, BK = 64, NBUF = 2;
+  static constexpr int P = 1, BK = 64;
 };
 template <>
 struct Tile<float> {
   typedef bf16_t E;
-  static constexpr int P = 3, BK = 32, NBUF = 1;
+  static constexpr int P = 3, BK = 32;
 };
 
 typedef bf16_t bf16x8 __attribute__((ext_vector_type(8)));
@@ -428,25 +428,28 @@ __device__ __forceinline__ void multiply(const char *la, const char *lb, int wi,
   }
 }
 
-// A block of 256 threads owns a TI x TJ tile, each wave a quarter of it in
-// blocks of 16 x 16.  The next K-tile is read into registers while this one is
-// multiplied.  Blocks go to the eight XCDs in turn: each XCD takes a run of
-// neighbouring tiles, of one part of k after the other, so that their operands
-// meet in its L2.
-// Tiles of 64 x 64 take K-tiles twice as long: what they lack is loads under way.
+// A block of 256 threads owns an S x S tile, each wave a quarter of it in blocks of
+// 16 x 16.  The next K-tile is read into registers while this one is multiplied.
+// Blocks go to the eight XCDs in turn: each XCD takes a run of neighbouring tiles,
+// of one part of k after the other, so that their operands meet in its L2 (dw of
+// 65,536 rows, 128 x 256, fp32, whose two tiles would otherwise keep to two XCDs: 122
+// -> 44 us).  Tiles of 64 x 64 take K-tiles twice as long: what they lack is loads
+// under way.  What bounds it, of floats: two barriers a K-tile with the splitting
+// between them, the matrix cores busy 53 % of the time: 65,536 x 1024 -> 1024 730 us,
+// 188 TFLOP/s (the library's fp32 product there 143); with the next K-tile stored
+// behind the products instead of ahead of them 815.
 template <class T, int S>
 struct RegTile {
   static constexpr int BK = S == 64 ? 2 * Tile<T>::BK : Tile<T>::BK;
-  static constexpr int NBUF = S == 64 ? 1 : Tile<T>::NBUF;
-  static constexpr int BYTES = NBUF * Tile<T>::P * 2 * S * BK * 2;
+  static constexpr int BYTES = Tile<T>::P * 2 * S * BK * 2;
 };
 template <class T, int S, bool IK, bool JK, bool HELD, bool LIN>
 __device__ __forceinline__ void gemm_body(const GemmArgs &a, char *lds, int64_t block) {
-  constexpr int TI = S, TJ = S, BK = RegTile<T, S>::BK, NBUF = RegTile<T, S>::NBUF;
+  constexpr int TI = S, TJ = S, BK = RegTile<T, S>::BK;
   typedef Operand<T, TI, IK, false, 256, BK> OA;
   typedef Operand<T, TJ, JK, HELD, 256, BK> OB;
-  constexpr int NI = TI / 32, NJ = TJ / 32, BUF = OA::BYTES + OB::BYTES;
-  const int lane = lane_id(), wave = threadIdx.x / WAVE;
+  constexpr int NI = TI / 32, NJ = TJ / 32;
+  const int wave = threadIdx.x / WAVE;
   const int wi = TI / 2 * (wave & 1), wj = TJ / 2 * (wave >> 1);
   const int64_t ti = (a.I + TI - 1) / TI, tj = (a.J + TJ - 1) / TJ, tiles = ti * tj;
   const int64_t units = tiles * a.parts, per = (units + 7) / 8;
@@ -470,32 +473,22 @@ __device__ __forceinline__ void gemm_body(const GemmArgs &a, char *lds, int64_t 
         fb.template fetch<false>(a.B, j0, a.J, k, k1, a.K);
       }
     };
-    auto stash = [&](int buf) {
-      fa.stash(lds + buf * BUF, 0);
-      fb.stash(lds + buf * BUF + OA::BYTES, a.B.hold);
+    auto stash = [&]() {
+      fa.stash(lds, 0);
+      fb.stash(lds + OA::BYTES, a.B.hold);
     };
     v4f acc[NI][NJ];
 #pragma unroll
     for (int i = 0; i < NI; ++i)
 #pragma unroll
       for (int j = 0; j < NJ; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
-    int buf = 0;
-    if (k0 < k1) {
-      fetch(k0);
-      __syncthreads();   // the tile before has been read
-      stash(0);
-      __syncthreads();
-    }
+    if (k0 < k1) fetch(k0);
     for (int64_t k = k0; k < k1; k += BK) {
-      const bool more = k + BK < k1;
-      if (more) fetch(k + BK);
-      multiply<OA, OB>(lds + buf * BUF, lds + buf * BUF + OA::BYTES, wi, wj, acc);
-      if (NBUF == 1) __syncthreads();
-      if (more) {
-        if (NBUF == 2) buf ^= 1;
-        stash(buf);
-        __syncthreads();
-      }
+      __syncthreads();   // the K-tile before, and the tile before, have been read
+      stash();
+      __syncthreads();
+      if (k + BK < k1) fetch(k + BK);
+      multiply<OA, OB>(lds, lds + OA::BYTES, wi, wj, acc);
     }
     __syncthreads();   // the last K-tile has been read
     write_tile<T, NI, NJ, IK, JK, HELD, LIN>(a, acc, lds + wave * 1024 * NJ, i0 + wi, j0 + wj,
@@ -563,7 +556,7 @@ __global__ void __launch_bounds__(256, 2) k_gemm_dma(GemmArgs a) {
     if (left >= BK) fetch(std::true_type{});
     else if (left > 0) fetch(std::false_type{});
   };
-  // the block's next unit from its u-th on (-1: none left), its first two K-tiles
+  // the block's next unit from its u-th on (-1: none left), its first NB - 1 K-tiles
   // asked for
   auto begin = [&](int64_t u) -> int64_t {
     for (; u < 8 * per; u += a.grid) {

