@@ -891,12 +891,29 @@ static bool direct(const LayerMat &m, int64_t width) {
 // ones by way of registers, which take half as long again for such rows, and twice
 // as long where they run along the side: us with copies / without, y of 65,536 x
 // 1001 -> 301 112 / 145, 2000 x 1001 -> 2001 31 / 44, its dx 34 / 62, dw 33 / 64; dw of
-// 16,384 x 333 -> 300 33 / 35
-static bool off_lines(int64_t width, int64_t ld) { return width % 8 != 0 || ld % 8 != 0; }
-static bool copies_pay(const Split &large, const Split &small, int prod, int copies,
+// 16,384 x 333 -> 300 33 / 35.  Rows that are off only because the matrix starts off
+// (all by the same bytes, their chunks whole) cost the small tiles less: 10 us and, next
+// to their estimate, 1.0 (y), 0.9 (dx) or 0.75 (dw) of it with one such operand, 1.3, 1.2
+// and 0.97 with two (measured at 17 sizes from 1000 x 2048 -> 2048 on).  us with copies /
+// without, of 16,384 x 1024 -> 1024: x off y 57 / 92, dw 55 / 97; w off y 48 / 84, dx 41 /
+// 82; all of them off 61 / 122, 52 / 120, 67 / 130; dw of 65,536 rows, 256 x 1024, x off
+// 102 / 90, of 100,000 rows, 128 x 512, 61 / 43
+enum { ON_LINES, OFF_START, OFF_ROWS };
+static int off_lines(const LayerMat &m, int64_t width) {
+  if (direct(m, width)) return ON_LINES;
+  LayerMat at0 = m;
+  at0.p = nullptr;
+  return direct(at0, width) ? OFF_START : OFF_ROWS;
+}
+static bool copies_pay(const Split &large, const Split &small, int prod, int off_a, int off_b,
                        int64_t elements) {
-  return large.us + 4.0 * copies + 8e-7 * (double)elements <
-         (prod == PROD_Y ? 1.4 : 2.0) * small.us;
+  static constexpr double rows[3] = {1.4, 2.0, 2.0}, one[3] = {1.0, 0.9, 0.75},
+                          two[3] = {1.3, 1.2, 0.97};   // by product
+  const int copies = (off_a != ON_LINES) + (off_b != ON_LINES);
+  const double without = off_a == OFF_ROWS || off_b == OFF_ROWS
+                             ? rows[prod] * small.us
+                             : 10.0 + (copies == 1 ? one[prod] : two[prod]) * small.us;
+  return large.us + 4.0 * copies + 8e-7 * (double)elements < without;
 }
 
 static int64_t tile_grid(const GemmArgs &a, int ti, int tj) {
@@ -960,22 +977,28 @@ static void gemm(GemmArgs &a, int side, hipStream_t s) {
 // Work space of the forward pass: copies of x and w with padded rows, and the parts
 struct LinearPlan {
   Split sp;
-  bool copy;
+  bool copy_x, copy_w;   // 16-bit operands of large tiles that cannot go straight into LDS
   size_t at_w, at_part, bytes;
 };
+static LayerMat plain_mat(const void *p, int64_t ld) { return LayerMat{p, ld, 0, nullptr, false}; }
 static LinearPlan linear_plan(const LinearArgs &a, int dtype) {
   LinearPlan p{};
   p.sp = split_of(a.m, a.n, a.k, dtype, PROD_Y);
-  if (dtype != NR_F32 && p.sp.side >= 128 && off_lines(a.k, a.ldx | a.ldw)) {
+  const int x_off = off_lines(plain_mat(a.x, a.ldx), a.k);
+  const int w_off = off_lines(plain_mat(a.w, a.ldw), a.k);
+  if (dtype != NR_F32 && a.m > 0 && p.sp.side >= 128 && (x_off || w_off)) {
     const Split small = split_of(a.m, a.n, a.k, dtype, PROD_Y, false);
-    p.copy = a.m > 0 && copies_pay(p.sp, small, PROD_Y, 2, (a.m + a.n) * a.k);
-    if (!p.copy) p.sp = small;
+    const bool pay = copies_pay(p.sp, small, PROD_Y, x_off, w_off,
+                                ((x_off ? a.m : 0) + (w_off ? a.n : 0)) * a.k);
+    p.copy_x = pay && x_off;
+    p.copy_w = pay && w_off;
+    if (!pay) p.sp = small;
   }
   const int64_t ldk = up(a.k, 32);
   size_t off = 0;
-  if (p.copy) off += up((size_t)a.m * ldk * 2, 256);
+  if (p.copy_x) off += up((size_t)a.m * ldk * 2, 256);
   p.at_w = off;
-  if (p.copy) off += up((size_t)a.n * ldk * 2, 256);
+  if (p.copy_w) off += up((size_t)a.n * ldk * 2, 256);
   p.at_part = off;
   p.bytes = off + part_bytes(p.sp, a.m, a.n);
   return p;
@@ -997,12 +1020,10 @@ static hipError_t linear_t(const LinearArgs &l, int dtype, char *ws, hipStream_t
   const LinearPlan p = linear_plan(l, dtype);
   GemmArgs a{};
   a.I = l.m, a.J = l.n, a.K = l.k;
-  a.A = LayerMat{l.x, l.ldx, 0, nullptr, false};
-  a.B = LayerMat{l.w, l.ldw, 0, nullptr, false};
-  if (p.copy) {
-    if (!direct(a.A, l.k)) a.A = padded<T>(l.x, l.ldx, l.m, l.k, ws, s);
-    if (!direct(a.B, l.k)) a.B = padded<T>(l.w, l.ldw, l.n, l.k, ws + p.at_w, s);
-  }
+  a.A = plain_mat(l.x, l.ldx);
+  a.B = plain_mat(l.w, l.ldw);
+  if (p.copy_x) a.A = padded<T>(l.x, l.ldx, l.m, l.k, ws, s);
+  if (p.copy_w) a.B = padded<T>(l.w, l.ldw, l.n, l.k, ws + p.at_w, s);
   a.lin = l;
   place(a, p.sp, ws + p.at_part);
   gemm<T, true, true, true>(a, p.sp.side, s);
@@ -1035,16 +1056,16 @@ static GradPlan grad_plan(const LinearGradArgs &a, int dtype) {
   if (a.dw) p.sw = split_of(a.n, a.k, a.m, dtype, PROD_DW);
   p.dz = a.act != NR_ACT_NONE && (a.dx || a.dw);
   const bool h16 = dtype != NR_F32 && a.m > 0;
-  const bool z_off = !p.dz && off_lines(a.n, a.lddy);
-  auto choose = [&](Split &sp, int64_t I, int J, int64_t K, int prod, bool off, int64_t elements) {
+  const int z_off = p.dz ? ON_LINES : off_lines(plain_mat(a.dy, a.lddy), a.n);
+  auto choose = [&](Split &sp, int64_t I, int J, int64_t K, int prod, int off, int64_t elements) {
     if (!h16 || sp.side < 128 || !(z_off || off)) return false;
     const Split small = split_of(I, J, K, dtype, prod, false);
-    if (copies_pay(sp, small, prod, z_off + off, (z_off ? a.m * a.n : 0) + (off ? elements : 0)))
+    if (copies_pay(sp, small, prod, z_off, off, (z_off ? a.m * a.n : 0) + (off ? elements : 0)))
       return true;
     sp = small;
     return false;
   };
-  const bool w_off = off_lines(a.k, a.ldw), x_off = a.x.hold || off_lines(a.k, a.x.ld);
+  const int w_off = off_lines(plain_mat(a.w, a.ldw), a.k), x_off = off_lines(a.x, a.k);
   const bool cx = a.dx && choose(p.sx, a.m, a.k, a.n, PROD_DX, w_off, (int64_t)a.n * a.k);
   const bool cw = a.dw && choose(p.sw, a.n, a.k, a.m, PROD_DW, x_off, a.m * a.k);
   p.copy_w = cx && w_off;
@@ -1089,11 +1110,10 @@ static hipError_t linear_grad_t(const LinearGradArgs &l, int dtype, char *ws, hi
     const dim3 g((unsigned)p.nb, (l.n + 8 * p.ct - 1) / (8 * p.ct));
     hipLaunchKernelGGL(k_act_grad<T>, g, dim3(ACT_THREADS), 0, s, l, p.rows, p.ct, dz, p.ldz, cols);
   }
-  const LayerMat z = p.dz ? LayerMat{dz, p.ldz, 0, nullptr, true}
-                          : LayerMat{l.dy, l.lddy, 0, nullptr, false};
+  const LayerMat z = p.dz ? LayerMat{dz, p.ldz, 0, nullptr, true} : plain_mat(l.dy, l.lddy);
   GemmArgs x{}, w{};
   x.I = l.m, x.J = l.k, x.K = l.n;
-  x.A = z, x.B = LayerMat{l.w, l.ldw, 0, nullptr, false};
+  x.A = z, x.B = plain_mat(l.w, l.ldw);
   x.out = l.dx, x.ldo = l.lddx;
   w.I = l.n, w.J = l.k, w.K = l.m;
   w.A = z, w.B = l.x;
@@ -1101,15 +1121,14 @@ static hipError_t linear_grad_t(const LinearGradArgs &l, int dtype, char *ws, hi
   const bool dx = l.dx && l.m > 0, dw = l.dw;
   if (dx) place(x, p.sx, ws + p.at_x);
   if (dw) place(w, p.sw, ws + p.at_w);
-  if (p.copy_w && !direct(x.B, l.k))
-    x.B = padded<T>(l.w, l.ldw, l.n, l.k, ws + p.at_cw, s);
+  if (p.copy_w) x.B = padded<T>(l.w, l.ldw, l.n, l.k, ws + p.at_cw, s);
   if (p.copy_x && l.x.hold) {
     const int64_t ld = up(l.k, 32);   // its padding is zeros
     const hipError_t e = launch_read((const uint8_t *)l.x.p, l.x.scale, l.m, (int)ld, l.x.hold,
                                      dtype, ws + p.at_cx, ld, s);
     if (e != hipSuccess) return e;
     w.B = LayerMat{ws + p.at_cx, ld, 0, nullptr, true};
-  } else if (p.copy_x && !direct(w.B, l.k)) {
+  } else if (p.copy_x) {
     w.B = padded<T>(l.x.p, l.x.ld, l.m, l.k, ws + p.at_cx, s);
   }
   if (dx && dw && p.sx.side == 64 && p.sw.side == 64) {
