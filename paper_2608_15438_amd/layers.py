@@ -6,7 +6,8 @@ Tensors are device tensors [..., width] of float32, bfloat16 or float16, all of
 a call's of one type.  `hold` ("i8" or "e4m3") keeps what the backward pass needs
 of the activations in 8 bits (nr_act_hold: a power of two per 32 elements): half
 of bfloat16's memory, a quarter of float32's; the gradients are then those of
-the held values.  Double backward is not supported.
+the held values.  Double backward is not supported.  Gradients have the tensors'
+type: in float16, whose smallest number is 6e-8, scale the loss (torch.amp.GradScaler).
 """
 from __future__ import annotations
 

@@ -109,7 +109,8 @@ class _Mlp(torch.nn.Module):
     """The encoder as trainable fp32 layers (ReLU between layers, the input
     scaled as at query time).  layers="hip" runs them on the library's kernels,
     in `dtype` (the parameters and the latents stay fp32) and with the activations
-    kept for the backward pass in 8 bits if `hold` says so."""
+    kept for the backward pass in 8 bits if `hold` says so.  In fp16 its gradients
+    need a scaled loss (train_encoder)."""
 
     def __init__(self, enc: Encoder, device, layers: str = "torch", dtype=torch.float32,
                  hold: Optional[str] = None):
@@ -159,10 +160,15 @@ def train_encoder(enc: Encoder, rows_fn: Callable, n: int, steps: int, batch: in
     """Adam on L_sim over seeded batches of rows drawn from [0, n) (the
     encoder has no BatchNorm; its biases and weights are trained).  layers="hip"
     runs the layers on the library's kernels in `dtype`, with the activations
-    held in 8 bits between the passes for hold="i8" or "e4m3"."""
+    held in 8 bits between the passes for hold="i8" or "e4m3".  In fp16 the loss
+    is scaled by a power of two: a step whose gradients leave the range all the
+    same is left out, and the scale halved."""
     dev = torch.device(device)
     net = _Mlp(enc, dev, layers, dtype, hold)
     opt = torch.optim.Adam(net.parameters(), lr=lr)
+    # L_sim is a mean over pairs: a latent's gradient is some 1e-5 and shrinks with the
+    # loss, where fp16's normal numbers end at 6e-5 and its last at 6e-8
+    scaler = torch.amp.GradScaler("cuda", enabled=dtype == torch.float16)
     g = torch.Generator(device="cpu").manual_seed(seed)
     for it in range(steps):
         ids = torch.randint(0, n, (batch,), generator=g)
@@ -172,8 +178,9 @@ def train_encoder(enc: Encoder, rows_fn: Callable, n: int, steps: int, batch: in
         fn = lsim_loss_gpu if dev.type == "cuda" else lsim_loss
         loss, tau, frac = fn(xs, lat, gamma, tau_emb, quantile)
         opt.zero_grad(set_to_none=True)
-        loss.backward()
-        opt.step()
+        scaler.scale(loss).backward()
+        scaler.step(opt)
+        scaler.update()
         if log and (it % max(1, steps // 10) == 0 or it == steps - 1):
             log(f"train step {it}: L_sim {float(loss.detach()):.5f}, tau_emb {tau:.4f}, "
                 f"mask {frac:.4%}")
