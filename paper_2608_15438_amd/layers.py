@@ -8,6 +8,8 @@ of the activations in 8 bits (nr_act_hold: a power of two per 32 elements): half
 of bfloat16's memory, a quarter of float32's; the gradients are then those of
 the held values.  Double backward is not supported.  Gradients have the tensors'
 type: in float16, whose smallest number is 6e-8, scale the loss (torch.amp.GradScaler).
+Under torch.no_grad() nothing is kept or put into 8 bits (needs_input_grad says which
+inputs want gradients there too, so the layers pass the grad mode on).
 """
 from __future__ import annotations
 
@@ -56,8 +58,8 @@ def _kept(ctx):
 
 class _Linear(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, w, bias, residual, act, hold):
-        need_x, need_w, need_b = ctx.needs_input_grad[:3]
+    def forward(ctx, x, w, bias, residual, act, hold, grad):
+        need_x, need_w, need_b = (need and grad for need in ctx.needs_input_grad[:3])
         x2 = _rows(x, "x")
         r2 = None if residual is None else _rows(residual, "residual")
         slope = act != "none" and (need_x or need_w or need_b)
@@ -89,14 +91,14 @@ class _Linear(torch.autograd.Function):
             dx, dw, db = NR.nr_linear_grad(d2, x2, w, act=ctx.act, pre=pre, dx=need_x, dw=need_w,
                                            db=need_b)
             dx = None if dx is None else dx.view(ctx.shape)
-        return dx, dw, db, dy if need_r else None, None, None
+        return dx, dw, db, dy if need_r else None, None, None, None
 
 
 class _LayerNorm(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight, bias, eps, hold):
+    def forward(ctx, x, weight, bias, eps, hold, grad):
         x2 = _rows(x, "x")
-        if any(ctx.needs_input_grad[:3]):
+        if grad and any(ctx.needs_input_grad[:3]):
             y, stats, *held = NR.nr_layer_norm(x2, weight, bias, eps, stats=True, hold_x=hold)
             _keep(ctx, held[0] if held else x2, stats, weight)
         else:
@@ -111,7 +113,7 @@ class _LayerNorm(torch.autograd.Function):
         need_x, need_w, need_b = ctx.needs_input_grad[:3]
         dx, dw, db = NR.nr_layer_norm_grad(_rows(dy, "dy"), x2, stats, weight, dx=need_x,
                                            dweight=need_w, dbias=need_b)
-        return None if dx is None else dx.view(ctx.shape), dw, db, None, None
+        return None if dx is None else dx.view(ctx.shape), dw, db, None, None, None
 
 
 def linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None,
@@ -124,7 +126,7 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias: Optional[torch.Tensor] = None
                          f"got {list(residual.shape)}")
     if hold is not None and hold not in NR.HOLDS:
         raise ValueError(f"hold must be one of {sorted(NR.HOLDS)}, got {hold!r}")
-    return _Linear.apply(x, w, bias, residual, act, hold)
+    return _Linear.apply(x, w, bias, residual, act, hold, torch.is_grad_enabled())
 
 
 def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None,
@@ -133,4 +135,4 @@ def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None,
     """Layer norm over the last dimension of x."""
     if hold is not None and hold not in NR.HOLDS:
         raise ValueError(f"hold must be one of {sorted(NR.HOLDS)}, got {hold!r}")
-    return _LayerNorm.apply(x, weight, bias, eps, hold)
+    return _LayerNorm.apply(x, weight, bias, eps, hold, torch.is_grad_enabled())
