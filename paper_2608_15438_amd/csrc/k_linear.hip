@@ -254,7 +254,8 @@ struct Operand {
     }
   }
   // (in asm, so that the compiler does not wait for them before every read of LDS;
-  // arrived() does, once a K-tile).  k of the chunks from `left` on: zeros
+  // arrived() does, once a K-tile.  m0 holds the LDS address; the load follows its
+  // writing by a wait state).  k of the chunks from `left` on: zeros
   template <bool FULL>
   static __device__ __forceinline__ void dma(const T *base, const uint32_t (&offset)[N],
                                              uint32_t lds, int left) {
@@ -262,14 +263,14 @@ struct Operand {
 #pragma unroll
     for (int u = 0; u < N; ++u) {
       if constexpr (FULL) {
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                     :: "s"(at + NT * 16 * u), "v"(offset[u]), "s"(base) : "memory");
+        asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                     :: "{m0}"(at + NT * 16 * u), "v"(offset[u]), "s"(base) : "memory");
       } else {
         const char *p = (const char *)base + offset[u];
         const int e = threadIdx.x + NT * u;
         if ((KC ? 8 * swap(e / CPR, e % CPR) : e / CPR) >= left) p = (const char *)&zero_chunk;
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
-                     :: "s"(at + NT * 16 * u), "v"(p) : "memory");
+        asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+                     :: "{m0}"(at + NT * 16 * u), "v"(p) : "memory");
       }
     }
   }
