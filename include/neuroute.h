@@ -317,7 +317,9 @@ nr_status nr_lsim_grad_at(const float *d2_emb, const float *lat, int64_t B, int3
  * fp32 and rounded to the type once; every result is the same bit for bit on
  * every call with the same inputs laid out the same.  fp32 products are made of
  * bf16 parts, good to 2^-24 of a product; an element below 2^-110 loses up to
- * 2^-126.  Outputs must not overlap inputs or one another.  Widths are 1..NR_MAX_WIDTH,
+ * 2^-126.  An fp32 output that comes out infinite or as no number is made again by
+ * plain fp32 products, one after the other: a call whose outputs are mostly so
+ * takes some 20 to 40 times as long.  Outputs must not overlap inputs or one another.  Widths are 1..NR_MAX_WIDTH,
  * rows >= 0 (0 rows: no output rows, and gradients of parameters are zero).
  * `ws` is DEVICE scratch of at least the bytes that the call's _ws function names
  * for the same description, pointers and strides included (16-byte aligned;

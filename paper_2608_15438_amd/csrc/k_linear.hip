@@ -294,29 +294,69 @@ struct Operand {
   }
 };
 
-// One output as a plain chain of fp32, for those that came out infinite or as no
-// number: the parts of an infinity (or of a float above the largest bf16) make
-// NaN of what is an infinity or a number
+// Eight neighbouring outputs of row i as plain chains of fp32 (the columns of `bad`;
+// the others stay as they are), for those that came out infinite or as no number: the
+// parts of an infinity (or of a float above the largest bf16) make NaN of what is an
+// infinity or a number.  The eight chains run side by side, with vector loads; all
+// that are no number end.  Slow all the same: 4096 x 1024 -> 1024 y 69 us, with every x
+// infinite 2800, one row of them 350; dw 69, with any row infinite (a term of every sum)
+// 1300
 template <bool IK, bool JK, bool HELD>
-__device__ float plain_chain(const LayerMat &A, const LayerMat &B, int64_t i, int j, int64_t k0,
-                             int64_t k1) {
-  float s = 0.0f;
+__device__ __forceinline__ void plain_chains(const LayerMat &A, const LayerMat &B, int64_t i,
+                                             int j, int J, int64_t k0, int64_t k1, uint32_t bad,
+                                             float (&v)[8]) {
+  float s[8] = {};
+#pragma unroll
+  for (int r = 0; r < 8; ++r) bad &= j + r < J ? ~0u : ~(1u << r);
+  auto open = [&]() {   // a wanted chain that may still change
+    bool o = false;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) o = o || ((bad >> r & 1) && s[r] == s[r]);
+    return o;
+  };
+  constexpr int U = JK ? 4 : 1;   // k at a time
 #pragma unroll 1
-  for (int64_t k = k0; k < k1; ++k) {
-    const float x = ((const float *)A.p)[IK ? i * A.ld + k : k * A.ld + i];
-    float w;
-    if constexpr (HELD) {
-      float v[4];
-      const uint8_t b = ((const uint8_t *)B.p)[k * B.ld + j];
-      hold_unpack4(b, hold_scale(B.scale[k * (B.ld / 32) + j / 32]), B.hold, v);
-      w = v[0];
+  for (int64_t k = k0; k < k1 && open(); k += U) {
+    int at = j;
+    // the addresses are found anew each time: kept over the loop they would cost
+    // registers that the products need
+    asm volatile("" : "+v"(at));
+    if constexpr (JK) {
+      static_assert(IK && !HELD, "both along k");
+      const float *a = (const float *)A.p + i * A.ld + k;
+      const bool whole = k + U <= k1;
+      float x[U] = {};
+      if (whole) __builtin_memcpy(x, a, sizeof x);
+      else
+        for (int u = 0; u < U - 1; ++u) x[u] = k + u < k1 ? a[u] : 0.0f;
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        const float *b = (const float *)B.p + (at + r < J ? at + r : J - 1) * B.ld + k;
+        if (whole) {
+          float w[U];
+          __builtin_memcpy(w, b, sizeof w);
+#pragma unroll
+          for (int u = 0; u < U; ++u) s[r] = fmaf(x[u], w[u], s[r]);
+        } else {
+          for (int u = 0; u < U - 1; ++u)
+            if (k + u < k1) s[r] = fmaf(x[u], b[u], s[r]);
+        }
+      }
     } else {
-      w = ((const float *)B.p)[JK ? j * B.ld + k : k * B.ld + j];
+      const float x = ((const float *)A.p)[IK ? i * A.ld + k : k * A.ld + i];
+      float w[8];
+      if constexpr (HELD) {   // (rows of whole groups)
+        unpack8<float>(*reinterpret_cast<const uint2 *>((const uint8_t *)B.p + k * B.ld + at),
+                       B.scale[k * (B.ld / 32) + at / 32], B.hold, w);
+      } else {
+        load8((const float *)B.p + k * B.ld, at, J, w);
+      }
+#pragma unroll
+      for (int r = 0; r < 8; ++r) s[r] = fmaf(x, w[r], s[r]);
     }
-    s = fmaf(x, w, s);
-    if (s != s) break;   // no number it stays
   }
-  return s;
+#pragma unroll
+  for (int r = 0; r < 8; ++r) v[r] = bad >> r & 1 ? s[r] : v[r];
 }
 
 // A wave's outputs, rows i0.. and columns j0.., or their parts' sums, sixteen rows at
@@ -367,18 +407,11 @@ __device__ __forceinline__ void write_tile(const GemmArgs &a, const v4f (&acc)[N
       float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
       const int64_t i = i0 + 16 * p + row;
       if constexpr (sizeof(T) == 4) {
-        bool bad = false;
+        uint32_t bad = 0;
 #pragma unroll
-        for (int r = 0; r < 8; ++r) bad = bad || !(fabsf(v[r]) < INFINITY);
-        if (bad && i < a.I) {
-#pragma unroll 1
-          for (int r = 0; r < 8; ++r)
-            if (j + r < a.J) {
-              const float o = plain_chain<IK, JK, HELD>(a.A, a.B, i, (int)j + r, k0, k1);
-#pragma unroll
-              for (int q = 0; q < 8; ++q) v[q] = q == r ? o : v[q];
-            }
-        }
+        for (int r = 0; r < 8; ++r) bad |= fabsf(v[r]) < INFINITY ? 0u : 1u << r;
+        if (bad && i < a.I)
+          plain_chains<IK, JK, HELD>(a.A, a.B, i, (int)j, a.J, k0, k1, bad, v);
       }
       if (a.part) {
         if (i < a.I && j < a.ldp) {
