@@ -778,7 +778,16 @@ constexpr int ACT_THREADS = 512;
 // dz = dy act'(pre) of `rows` rows per block, rounded to the type, zeros from n up to
 // ldz (a multiple of 32; dz NULL: not wanted), and its column sums over them (part
 // NULL: not wanted).  The threads are ACT_THREADS / ct rows of ct threads, eight
-// columns each
+// columns each.
+// The rounding of dz is a choice.  In the 16-bit types it is an operand of the matrix
+// cores, which take 16 bits, as every tensor of such a network between two of its
+// layers is; the column sums take it unrounded.  It adds one rounding of independent
+// size to that of the outputs themselves: dx and dw of a bf16 gelu layer are 0.0024 off
+// in the 2-norm (fp16 0.00030), where rounding exact ones gives 0.0017 (0.00021); z, kept in
+// the type too, has 0.0001 of that.  dz in two parts (it and the rest, both in the type),
+// was measured: 0.0017 again, for 16,384 x 1024 -> 1024 with gelu 108 -> 167 us, 65,536 x
+// 1024 -> 4096 1306 -> 2302, in the product of dx alone 111 -> 147 and 1330 -> 1970.  With no
+// activation and with relu dz is exact (dy or 0)
 template <class T>
 __global__ void __launch_bounds__(ACT_THREADS) k_act_grad(LinearGradArgs a, int64_t rows, int ct,
                                                           T *dz, int64_t ldz, float *part) {

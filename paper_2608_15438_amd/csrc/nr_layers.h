@@ -205,7 +205,8 @@ __device__ __forceinline__ void hold_unpack4(uint32_t w, float s, int hold, floa
   }
 }
 
-// eight held elements, as the type has them (fp16's subnormals round)
+// eight held elements, as the type has them: fp16's subnormals round, so that a kernel
+// that reads what is held in place finds the values of the tensor that reads it out
 template <class T>
 __device__ __forceinline__ void unpack8(uint2 w, uint8_t scale, int hold, float (&v)[8]) {
   const float s = hold_scale(scale);
@@ -278,6 +279,8 @@ __device__ __forceinline__ float normal_cdf(float z, float &e) {
   }
 }
 
+// The 16-bit types take the hardware's exponential and reciprocal (a few 2^-23 of the
+// result; half a step of fp16 is 2^-12 of it), fp32 the library's
 template <bool EXACT>
 __device__ __forceinline__ float logistic(float z) {
   if constexpr (EXACT) return 1.0f / (1.0f + expf(-z));
