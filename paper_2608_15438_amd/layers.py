@@ -5,11 +5,14 @@ run with (its latents go to Index.nr_search as `logits`).
 Tensors are device tensors [..., width] of float32, bfloat16 or float16, all of
 a call's of one type.  `hold` ("i8" or "e4m3") keeps what the backward pass needs
 of the activations in 8 bits (nr_act_hold: a power of two per 32 elements): half
-of bfloat16's memory, a quarter of float32's; the gradients are then those of
-the held values.  Double backward is not supported.  Gradients have the tensors'
-type: in float16, whose smallest number is 6e-8, scale the loss (torch.amp.GradScaler).
-Under torch.no_grad() nothing is kept or put into 8 bits (needs_input_grad says which
-inputs want gradients there too, so the layers pass the grad mode on).
+of bfloat16's memory, a quarter of float32's.  A linear layer's gradients are then
+those at the held values; a layer norm's take the held row with the mean and the
+deviation of the row itself, which it keeps in fp32.  Under torch.no_grad() nothing
+is kept or put into 8 bits (needs_input_grad says which inputs want gradients there
+too, so the layers pass the grad mode on).
+
+Gradients have the tensors' type: in float16, whose smallest number is 6e-8, scale
+the loss (torch.amp.GradScaler).  Double backward is not supported.
 """
 from __future__ import annotations
 
