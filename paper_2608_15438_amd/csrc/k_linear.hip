@@ -469,9 +469,10 @@ __device__ __forceinline__ void multiply(const char *la, const char *lb, int wi,
 // 65,536 rows, 128 x 256, fp32, whose two tiles would otherwise keep to two XCDs: 122
 // -> 44 us).  Tiles of 64 x 64 take K-tiles twice as long: what they lack is loads
 // under way.  What bounds it, of floats: two barriers a K-tile with the splitting
-// between them, the matrix cores busy 53 % of the time: 65,536 x 1024 -> 1024 730 us,
-// 188 TFLOP/s (the library's fp32 product there 143); with the next K-tile stored
-// behind the products instead of ahead of them 815.
+// between them, the matrix cores busy 53 % of the cycles: 65,536 x 1024 -> 1024 730 to
+// 757 us, 182 to 188 TFLOP/s (the library's fp32 product there 142); with the next
+// K-tile stored behind the products instead of ahead of them 815.  (A held operand's
+// second and third parts are zero and multiplied all the same.)
 template <class T, int S>
 struct RegTile {
   static constexpr int BK = S == 64 ? 2 * Tile<T>::BK : Tile<T>::BK;
@@ -550,13 +551,16 @@ __global__ void __launch_bounds__(256, 2) k_gemm_two(GemmArgs x, GemmArgs w) {
 // epilogue, while the other multiplies; a block goes on to its next tile with that
 // tile's first K-tiles already under way.  128 x 128 tiles take k 64 at a time, whole
 // lines of rows that run along k (32 at a time the 8192^3 product took 1053 us, 64
-// 945, the library 692 to 708); 256 x 128 tiles, two thirds of the traffic, take 32, for
+// 945, the library 679 to 707); 256 x 128 tiles, two thirds of the traffic, take 32, for
 // products with an operand that runs along its side (dw of 65,536 rows, 4096 x 1024:
-// 442 us, 1.24 PFLOP/s; in 128 x 128 517).  What bounds it: matrix instructions half
-// of the time, at clocks of 2.0 of 2.4 GHz; the rest are waits for operands.  Tried
-// and slower: one block of eight waves, 256 x 256, operands half a K-tile ahead (1141
-// TFLOP/s at k = 8192, but its epilogue stands alone: 740 us for 65,536 x 1024 ->
-// 4096, now 620); operands from LDS a K-tile ahead with 128 x 128 tiles (1003 / 945 us)
+// 443 us, 1.24 PFLOP/s, and a join of 8; in 128 x 128 549 with the join.  Its kernel spills
+// 24 B a lane at 256 registers).  What bounds it is waits for operands, and the
+// epilogue: the matrix cores are busy 40 % of the cycles in 65,536 x 1024 -> 4096, 35 %
+// with bias and gelu, 50 % in its dx, 74 % in its dw and 68 % in 8192^3 (the library's
+// kernel 93 %), at 1.6 to 2.0 of 2.4 GHz.  Tried and slower: one block of eight waves, 256
+// x 256, operands half a K-tile ahead (1141 TFLOP/s at k = 8192, but its epilogue
+// stands alone: 740 us for 65,536 x 1024 -> 4096, here 645 to 670); operands from LDS a
+// K-tile ahead with 128 x 128 tiles (1003 / 945 us)
 template <class T, int TI, int TJ, int BK, int NB, bool IK, bool JK, bool LIN>
 __global__ void __launch_bounds__(256, 2) k_gemm_dma(GemmArgs a) {
   constexpr int NI = TI / 32, NJ = TJ / 32;
@@ -866,12 +870,12 @@ static bool aligned(const void *p, int64_t ld, size_t e, size_t to) {
 // CU, at `alone` / 256 where it has one to itself, but at least `step` for each
 // K-tile of bk, and all of them together the operands' bytes at `stream` TB/s;
 // parts cost a launch, and their sums' way through memory.  Measured, us, the
-// chosen one last: y of 10,000 x 1536 -> 512 fp32 in 128 x 128 168, 64 x 64 137, 128 x
-// 128 in four parts 124; bf16 700 x 2000 -> 900 64 x 64 39, 128 x 128 26, in four parts
-// 19; 4096 x 512 -> 512 128 x 128 13, 64 x 64 9.8; 48 x 4096 -> 4096 64 x 64 in eight
-// parts 20, 128 x 128 in eight 15.6; 16,384 x 512 -> 512 64 x 64 24, 128 x 128 17.5; dx of
-// 65,536 x 4096 -> 1024 128 x 128 608, 256 x 128 560; dw of 65,536 rows, 4096 x 1024, 128 x
-// 128 in two parts 517, 256 x 128 in four 501
+// chosen one last: y of 10,000 x 1536 -> 512 fp32 in 128 x 128 156, 64 x 64 129, 128 x
+// 128 in four parts 114; bf16 700 x 2000 -> 900 64 x 64 36, 128 x 128 25, in four parts
+// 18; 4096 x 512 -> 512 128 x 128 13, 64 x 64 9.5; 48 x 4096 -> 4096 64 x 64 in eight
+// parts 18.6, 128 x 128 in eight 14.7; 16,384 x 512 -> 512 64 x 64 24, 128 x 128 17.4; dx of
+// 65,536 x 4096 -> 1024 128 x 128 578, 256 x 128 560; dw of 65,536 rows, 4096 x 1024, 128 x
+// 128 in two parts 549, 256 x 128 in four 452
 enum { PROD_Y, PROD_DX, PROD_DW };
 struct Split {
   int side, parts;
@@ -927,14 +931,14 @@ static bool direct(const LayerMat &m, int64_t width) {
 }
 
 // Rows that lie off the 16-byte boundaries can be read, but not straight into LDS,
-// and a load across two lines costs two: us of bf16 products at widths of 1024 /
-// 1023, 16,384 rows: y 50 / 73, dx 38 / 94, dw 61 / 111.  So 16-bit operands are
+// and a load across two lines costs two: us of bf16 products in 64 x 64 tiles at widths
+// of 1024 / 1023, 16,384 rows: y 70 / 119, dx 74 / 108, dw 71 / 170.  So 16-bit operands are
 // copied to padded rows first (k_pad_rows: 4 us, and 4 bytes an element at some 5
 // TB/s) where large tiles with the copies are estimated to be faster than small
 // ones by way of registers, which take half as long again for such rows, and twice
 // as long where they run along the side: us with copies / without, y of 65,536 x
 // 1001 -> 301 112 / 145, 2000 x 1001 -> 2001 31 / 44, its dx 34 / 62, dw 33 / 64; dw of
-// 16,384 x 333 -> 300 33 / 35.  Rows that are off only because the matrix starts off
+// 16,384 x 333 -> 300 33 / 34.  Rows that are off only because the matrix starts off
 // (all by the same bytes, their chunks whole) cost the small tiles less: 10 us and, next
 // to their estimate, 1.0 (y), 0.9 (dx) or 0.75 (dw) of it with one such operand, 1.3, 1.2
 // and 0.97 with two (measured at 17 sizes from 1000 x 2048 -> 2048 on).  us with copies /

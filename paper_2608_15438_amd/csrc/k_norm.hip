@@ -8,7 +8,10 @@
 // registers too, over all the rows that a group of lanes takes; a block's groups
 // meet in LDS, the blocks' sums in a second kernel, in a fixed order.  65,536 x 1536
 // bf16: forward 77 us (403 MB, 5.2 TB/s), backward with `add` 178 and 7 for the
-// column sums (805 MB, 4.5 TB/s).
+// column sums (805 MB, 4.5 TB/s).  Rows wider than 8192 take 64 elements a lane, and
+// their backward kernel spills 196 B a lane (16 bits 44): 8192 rows of 16,384 fp32 220 us
+// forward, 449 backward (4.9 and 3.6 TB/s), bf16 163 and 370; of 8192 98 and 177, 52 and
+// 180.
 #include <type_traits>
 
 #include "nr_layers.h"
